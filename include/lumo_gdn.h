@@ -14,7 +14,9 @@
  * lumo_select_spine_top3 (fused draft selection upstream of the tree), lumo_gdn_tree_scan_static
  * (the scan with library-internal static scratch), the attention half of the same cycle
  * (lumo_kv_write_tree, lumo_tree_attention, lumo_kv_publish: the tree's KV entries written, read and
- * re-linearised through the same slot map) and small helpers.
+ * re-linearised through the same slot map) and small helpers.  The attention half also runs over a paged cache held in 4 bits
+ * (lumo_kv4_*), with the norm and rotation of queries and keys in front of it (lumo_qk_norm_rope) and the bookkeeping of its pages
+ * (lumo_pages_*, lumo_rows_copy).
  *
  * Conventions
  *   - One GPU.  All tensor pointers are DEVICE pointers owned by the caller unless a
@@ -65,7 +67,9 @@ typedef enum {
   LUMO_SEQ_BAD_LINK = 4,  /* accepted entry t is not a child of entry t-1 */
   LUMO_SEQ_BAD_ROW = 5,   /* state_row[b] >= n_state_rows */
   LUMO_SEQ_TIMEOUT = 6,   /* a bounded device-side wait ran out; outputs of the call are invalid */
-  LUMO_SEQ_BAD_CTX = 7    /* attention calls: ctx_len[b] < 0 or ctx_len[b] + Ns > max_positions */
+  LUMO_SEQ_BAD_CTX = 7,   /* attention calls: ctx_len[b] < 0 or ctx_len[b] + Ns > max_positions; page calls: a length out of range */
+  LUMO_SEQ_BAD_PAGE = 8,  /* paged calls: a page that is needed does not exist (or, for a write, is shared) */
+  LUMO_SEQ_NO_PAGES = 9   /* lumo_pages_reserve: the free pages do not suffice; nothing was changed */
 } lumo_seq_status;
 
 /* Integer tables of one tree (lumo_tree_desc_get).  The paper's tree descriptor holds parent
@@ -163,7 +167,9 @@ int lumo_ctx_set_overlap(lumo_ctx* ctx, int on);
  * records.  Enabling allocates the event pool; do not enable inside a stream capture. */
 typedef enum { LUMO_K_CONV = 0, LUMO_K_SCAN = 1, LUMO_K_COMMIT = 2, LUMO_K_PATH = 3,
                LUMO_K_ATTN = 4, LUMO_K_ATTN_MERGE = 5, LUMO_K_KV_WRITE = 6, LUMO_K_KV_PUBLISH = 7,
-               LUMO_K_COUNT = 8 } lumo_kernel_kind;
+               LUMO_K_ROPE = 8, LUMO_K_KV4_WRITE = 9, LUMO_K_KV4_READ = 10, LUMO_K_KV4_PUBLISH = 11, LUMO_K_KV4_ATTN = 12,
+               LUMO_K_KV4_MERGE = 13, LUMO_K_PAGES = 14, LUMO_K_ROWS_COPY = 15,
+               LUMO_K_COUNT = 16 } lumo_kernel_kind;
 int lumo_ctx_timing_enable(lumo_ctx* ctx, int enable);
 int lumo_ctx_timing_read(lumo_ctx* ctx, int kind, int reset, int64_t* launches, double* total_ms);
 
@@ -424,6 +430,139 @@ int lumo_tree_attention(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_at
 int lumo_kv_publish(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_attn_args* layers, int n_layers,
                     const int32_t* accepted_dev, const int32_t* len_dev, int lmax, int32_t* ctx_len_out,
                     void* stream);
+
+/* ---- norm and rotation of queries and keys -----------------------------------------------
+ * What stands between a full-attention layer's projection and its cache, in one pass over every head of every token:
+ *   y = x / sqrt(mean(x^2) + eps) * (w + weight_offset)      (normalise = 1; w = 1 where the weight is NULL)
+ *   pair j of y's first `rot` elements: (a, b) -> mscale (a cos t - b sin t, a sin t + b cos t),  t = position * inv_freq[j]
+ * Sums and products in fp32, angles reduced in 64 bits, one rounding at the end.  style 0: the pair of element j < rot / 2 is
+ * element j + rot / 2; style 1: pairs are elements (2 j, 2 j + 1).  Elements at and beyond rot are not rotated.
+ * Positions: pos [axes, T]; with axes = 3 (time, height, width of pictures and video) the pairs are dealt out to the axes, either in three
+ * blocks of section[0], section[1], section[2] pairs (turns = 0), or by turns (turns = 1: pair j belongs to axis j mod 3 while
+ * j / 3 < section[j mod 3] for axes 1 and 2, else to axis 0); the sections add up to rot / 2.  pos = NULL: the tokens are the nodes of
+ * desc's trees in logical order (T = B N) and a node's position is ctx_len[b] + depth - 1.
+ * q, k: [T, heads, dh], heads adjacent, *_stride elements from token to token (0: heads * dh), so that parts of a packed projection can
+ * be passed as they are; q_out, k_out likewise.  An output may be its input (same pointer and stride); any other overlap is undefined.
+ * dh 64, 128 or 256; rot a multiple of 16, 0 to dh; Hkv may be 0 (k and k_out unused). */
+typedef struct {
+  int32_t T, Hq, Hkv, dh;
+  int32_t dtype;           /* lumo_dtype of q, k, their outputs and weights */
+  int32_t rot, style;
+  int32_t axes, turns;     /* axes 1 or 3 */
+  int32_t section[3];
+  int32_t normalise;
+  float eps, weight_offset, mscale;
+  const void* q; const void* k;
+  void* q_out; void* k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  const void* q_weight; const void* k_weight;   /* [dh] or NULL */
+  const float* inv_freq;   /* [rot / 2] */
+  const int32_t* pos;      /* [axes, T] or NULL */
+  const int32_t* ctx_len;  /* [B], read when pos is NULL */
+} lumo_qk_args;
+int lumo_qk_norm_rope(lumo_ctx* ctx, const lumo_tree_desc* desc /* may be NULL with pos */, const lumo_qk_args* args, void* stream);
+
+/* ---- the attention half over a paged cache held in 4 bits ---------------------------------
+ * A head's key (or value) of one position is eight blocks of 16 numbers.  A block is an e4m3 scale s (8 bits) and sixteen e2m1 codes
+ * c (4 bits) and stands for c s 2^e; e is k_exp for keys and v_exp for values.  Written from bf16:
+ *   s = e4m3(max|x| 2^-e / 6), nearest, ties to even, at most 448;  c = e2m1(x 2^-e / s), nearest, ties to the even code, at most 6;
+ *   a block whose scale rounds to 0 holds zeros, a block with a NaN holds NaN (scale NaN), infinities count as the largest value.
+ * One page holds page_size positions of all KV heads: pages [n_pages, Hkv, 2 (keys, values), page_size * 72] bytes, and in each 72 *
+ * page_size first the codes [page_size, 64] (element 2 i in the low half of byte i), then the scales [page_size, 8].
+ * table [n_rows, max_pages]: page number of each page_size positions of a cache row, -1 = none (lumo_pages_* keep such a table; any other
+ * way to fill it will do).  Rows, contexts, the slot map and visibility are those of the bf16 calls above: sequence b owns
+ * row cache_row[b], the entry of node i lies at position ctx_len[b] + slot[b][i], with max_positions = max_pages * page_size.
+ * Status per sequence: LUMO_SEQ_BAD_ROW, LUMO_SEQ_BAD_CTX as above, and LUMO_SEQ_BAD_PAGE when a page that the call needs is not in
+ * [0, n_pages); with refs given, a write or publication also refuses a page whose count is not 1.  Such a sequence is left as it
+ * was (write, publish) or gets zero outputs and lse (attention).  Supported: dh = 128, page_size 16, 32, 64 or 128, Ns <= 256,
+ * n_layers <= 32, B <= 65535. */
+typedef struct {
+  int32_t Hq, Hkv, dh;
+  float scale;              /* logits = scale * q . k */
+  int32_t n_rows, max_pages, n_pages, page_size;
+  int32_t k_exp, v_exp;     /* -24 .. 24 */
+  void* pages;              /* the layer's pool */
+  const int32_t* table;
+  const int32_t* refs;      /* [n_pages] or NULL */
+  const int32_t* ctx_len;   /* [B] */
+  const int32_t* cache_row; /* [B] */
+  const void* q;            /* [B, N, Hq, dh] bf16 (attention) */
+  const void* k_new;        /* [B, N, Hkv, dh] bf16 (tree write), [T, Hkv, dh] (append) */
+  const void* v_new;
+  int64_t q_stride, kv_stride;  /* elements from token to token; 0: heads * dh */
+  void* out;                /* [B, N, Hq, dh] (attention) */
+  int32_t out_dtype;        /* lumo_dtype of out */
+  float* lse;               /* [B, N, Hq] fp32 or NULL */
+  int32_t n_splits;         /* as in lumo_attn_args */
+  int32_t* status;          /* [B] (append: [T]); may be NULL */
+  void* work;               /* attention: lumo_kv4_work_bytes bytes; calls that share it must not overlap */
+  int64_t work_bytes;
+} lumo_kv4_args;
+
+/* The tree's entries, quantised and written through the slot map.  A sequence is written whole or not at all. */
+int lumo_kv4_write_tree(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, void* stream);
+/* Tokens listed one by one (a prompt): entry of token t goes to position tok_pos[t] of row tok_row[t]; row -1 is passed over.  The
+ * (row, position) pairs of a call must be distinct.  status [T].  ctx_len and cache_row are not read.  T * Hkv < 2^30. */
+int lumo_kv4_append(lumo_ctx* ctx, const lumo_kv4_args* layers, int n_layers, int T, const int32_t* tok_row, const int32_t* tok_pos,
+                    void* stream);
+/* The listed tokens' entries of one layer as bf16 [T, Hkv, dh] (exact while 2^e keeps them in range); zeros for a token that is passed
+ * over or refused.  status [T]. */
+int lumo_kv4_read(lumo_ctx* ctx, const lumo_kv4_args* layer, int T, const int32_t* tok_row, const int32_t* tok_pos, void* k_out, void* v_out,
+                  void* stream);
+/* Bytes of workspace lumo_kv4_attention needs for these trees, heads and splits (0 on a bad argument). */
+int64_t lumo_kv4_work_bytes(const lumo_ctx* ctx, const lumo_tree_desc* desc, int Hq, int Hkv, int n_splits);
+/* lumo_tree_attention over the 4-bit pages.  Codes times scales are exact in f16; probabilities enter the second product rounded to
+ * f16; all sums are fp32.  A NaN held in a page reaches the outputs of the nodes that see its position and no others; bytes of
+ * positions that nobody sees may be anything.  Bitwise reproducible for a given device, shape and n_splits.  Enqueues only and
+ * allocates nothing; partial results live in `work`, which the layers of a call use one after another. */
+int lumo_kv4_attention(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, void* stream);
+/* lumo_kv_publish over the 4-bit pages: the accepted entries move as they are, bit for bit. */
+int lumo_kv4_publish(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, const int32_t* accepted_dev,
+                     const int32_t* len_dev, int lmax, int32_t* ctx_len_out, void* stream);
+
+/* ---- pages ---------------------------------------------------------------------------------
+ * Bookkeeping of a paged cache on the device, for rows of any kind of page: every pool (one per layer, say) is an array of n_pages pages of
+ * page_bytes bytes, numbered alike.  Row r holds pages table[r][0 .. row_pages[r]); the rest of its table is -1.  refs counts the table
+ * entries that name a page; free_list[0 .. free_count) are the others, the next one to be taken last.
+ * The calls list rows of the table by device arrays of n entries (1 to 1024; row -1 is passed over) and work through the list in its order:
+ * results follow from the list and the tables alone.  A row listed twice is refused the second time (LUMO_SEQ_BAD_ROW), like
+ * one outside the table; status [n] (may be NULL) has a word per entry.  Calls on one table must not overlap. */
+typedef struct {
+  int32_t n_rows, max_pages, n_pages, page_size;   /* page_size: positions of a page, 1 to 4096; max_pages, n_pages <= 262144 */
+  int32_t* table;          /* [n_rows, max_pages] */
+  int32_t* row_pages;      /* [n_rows] */
+  int32_t* refs;           /* [n_pages] */
+  int32_t* free_list;      /* [n_pages] */
+  int32_t* free_count;     /* [1] */
+  int32_t* work;           /* lumo_pages_work_ints(n_rows, n_pages) ints of scratch */
+  int32_t n_pools;         /* 0 to 64 */
+  void* const* pools;      /* HOST array of device pointers, 16-byte aligned */
+  int64_t page_bytes;      /* a multiple of 16 */
+} lumo_page_table;
+int64_t lumo_pages_work_ints(int n_rows, int n_pages);
+/* Empty rows, all pages free (page 0 is taken first). */
+int lumo_pages_init(lumo_ctx* ctx, const lumo_page_table* t, void* stream);
+/* Row dst[i], which holds no pages, shares all pages of row src[i].  A dst that an earlier pair names, or that is a source of the call, is
+ * refused. */
+int lumo_pages_fork(lumo_ctx* ctx, const lumo_page_table* t, const int32_t* src, const int32_t* dst, int n, int32_t* status, void* stream);
+/* Makes positions [start[i], end[i]) of row rows[i] writable (end = NULL: end[i] = start[i] + add): pages among them that other rows share
+ * are replaced by copies in all pools, missing ones up to end are added (with whatever bytes they hold).  When all sharers of a page
+ * are listed, the last of them keeps it.  Pages come off the list in the order of the rows, a row's copies before its additions.
+ * When the free pages do not suffice for the whole call, nothing changes and every row gets LUMO_SEQ_NO_PAGES. */
+int lumo_pages_reserve(lumo_ctx* ctx, const lumo_page_table* t, const int32_t* rows, const int32_t* start, const int32_t* end, int add,
+                       int n, int32_t* status, void* stream);
+/* Gives back the pages of row rows[i] that lie wholly behind its first keep[i] positions (keep = NULL: all).  A page that no row holds any
+ * longer becomes free; the pages that a call frees are stored last one first, so that a following reserve of the same rows takes them in
+ * the same order. */
+int lumo_pages_free(lumo_ctx* ctx, const lumo_page_table* t, const int32_t* rows, const int32_t* keep, int n, int32_t* status, void* stream);
+/* Moves the pages in use to the lowest numbers, in all pools and tables: with L pages in use, the k-th of them at or beyond number L
+ * goes to the k-th unused number below L.  The free list becomes n_pages - 1 down to L (L is taken first). */
+int lumo_pages_compact(lumo_ctx* ctx, const lumo_page_table* t, void* stream);
+/* Rows of caches that are not paged (recurrent states, convolution histories): row src[i] of every block copied to row dst[i].  blocks:
+ * HOST array of n_blocks (1 to 64) device arrays of n_rows rows, row_bytes[j] bytes each (HOST array; multiples of 16).  A dst that an
+ * earlier pair names, or that is a source of the call, is refused; row -1 is passed over. */
+int lumo_rows_copy(lumo_ctx* ctx, void* const* blocks, const int64_t* row_bytes, int n_blocks, int n_rows, const int32_t* src,
+                   const int32_t* dst, int n, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

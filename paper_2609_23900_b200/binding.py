@@ -25,20 +25,25 @@ _lib = ctypes.CDLL(LIB_PATH)
 LUMO_F32, LUMO_BF16 = 0, 1
 _DTYPE = {torch.float32: LUMO_F32, torch.bfloat16: LUMO_BF16}
 
-SEQ_OK, SEQ_BAD_LEN, SEQ_BAD_NODE, SEQ_BAD_ROOT, SEQ_BAD_LINK, SEQ_BAD_ROW, SEQ_TIMEOUT, SEQ_BAD_CTX = range(8)
+(SEQ_OK, SEQ_BAD_LEN, SEQ_BAD_NODE, SEQ_BAD_ROOT, SEQ_BAD_LINK, SEQ_BAD_ROW, SEQ_TIMEOUT, SEQ_BAD_CTX, SEQ_BAD_PAGE,
+ SEQ_NO_PAGES) = range(10)
 
 TABLES = ["depth", "n_child", "child_off", "child_list", "is_leaf", "leaves", "path_off", "path_nodes",
           "anc_win", "slot_inv", "chain_head", "chain_off", "chain_nodes", "chain_level", "cut_nodes",
           "schedule", "schedule_full", "gram_groups", "attn_vis"]
 
-KERNEL_KINDS = ["conv", "scan", "commit", "path", "attn", "attn_merge", "kv_write", "kv_publish"]
+KERNEL_KINDS = ["conv", "scan", "commit", "path", "attn", "attn_merge", "kv_write", "kv_publish",
+                "rope", "kv4_write", "kv4_read", "kv4_publish", "kv4_attn", "kv4_merge", "pages", "rows_copy"]
 
 EXPORTS = ["lumo_ctx_create", "lumo_ctx_destroy", "lumo_last_error", "lumo_ctx_scratch_bytes",
            "lumo_ctx_timing_enable", "lumo_ctx_timing_read", "lumo_ctx_set_scan_algo", "lumo_ctx_set_overlap", "lumo_ctx_set_timeout_drill",
            "lumo_tree_desc_create", "lumo_tree_desc_destroy", "lumo_tree_desc_get",
            "lumo_tree_path_from_node", "lumo_gdn_tree_verify", "lumo_gdn_commit",
            "lumo_gdn_tree_scan_static", "lumo_static_stack_bytes", "lumo_conv_rows_per_cta", "lumo_tree_accept", "lumo_select_spine_top3", "lumo_gdn_commit_verify",
-           "lumo_kv_write_tree", "lumo_tree_attention", "lumo_kv_publish"]
+           "lumo_kv_write_tree", "lumo_tree_attention", "lumo_kv_publish",
+           "lumo_qk_norm_rope", "lumo_kv4_write_tree", "lumo_kv4_append", "lumo_kv4_read", "lumo_kv4_work_bytes", "lumo_kv4_attention",
+           "lumo_kv4_publish", "lumo_pages_work_ints", "lumo_pages_init", "lumo_pages_fork", "lumo_pages_reserve", "lumo_pages_free",
+           "lumo_pages_compact", "lumo_rows_copy"]
 
 
 class LumoError(RuntimeError):
@@ -91,6 +96,36 @@ class _AttnArgs(ctypes.Structure):
                 ("kv_layout", ctypes.c_int32), ("n_splits", ctypes.c_int32), ("status", ctypes.c_void_p)]
 
 
+class _QkArgs(ctypes.Structure):
+    """Mirror of lumo_qk_args."""
+    _fields_ = [("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("dh", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("rot", ctypes.c_int32), ("style", ctypes.c_int32), ("axes", ctypes.c_int32), ("turns", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3), ("normalise", ctypes.c_int32), ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float),
+                ("mscale", ctypes.c_float), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("ctx_len", ctypes.c_void_p)]
+
+
+class _Kv4Args(ctypes.Structure):
+    """Mirror of lumo_kv4_args."""
+    _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("dh", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("k_exp", ctypes.c_int32), ("v_exp", ctypes.c_int32), ("pages", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("ctx_len", ctypes.c_void_p), ("cache_row", ctypes.c_void_p), ("q", ctypes.c_void_p),
+                ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("kv_stride", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_dtype", ctypes.c_int32), ("lse", ctypes.c_void_p), ("n_splits", ctypes.c_int32),
+                ("status", ctypes.c_void_p), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_int64)]
+
+
+class _PageTableArgs(ctypes.Structure):
+    """Mirror of lumo_page_table."""
+    _fields_ = [("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("row_pages", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("free_list", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p), ("work", ctypes.c_void_p), ("n_pools", ctypes.c_int32), ("pools", ctypes.c_void_p),
+                ("page_bytes", ctypes.c_int64)]
+
+
 _lib.lumo_ctx_create.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_void_p)]
 _lib.lumo_ctx_destroy.argtypes = [ctypes.c_void_p]
 _lib.lumo_ctx_destroy.restype = None
@@ -136,6 +171,27 @@ _lib.lumo_kv_publish.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTE
                                  ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
 
 
+_lib.lumo_qk_norm_rope.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(_QkArgs), ctypes.c_void_p]
+for _f in (_lib.lumo_kv4_write_tree, _lib.lumo_kv4_attention):
+    _f.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_void_p]
+_lib.lumo_kv4_append.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                 ctypes.c_void_p]
+_lib.lumo_kv4_read.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int] + [ctypes.c_void_p] * 5
+_lib.lumo_kv4_work_bytes.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_int]
+_lib.lumo_kv4_work_bytes.restype = ctypes.c_int64
+_lib.lumo_kv4_publish.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                  ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
+_lib.lumo_pages_work_ints.argtypes = [ctypes.c_int, ctypes.c_int]
+_lib.lumo_pages_work_ints.restype = ctypes.c_int64
+_lib.lumo_pages_init.argtypes = [ctypes.c_void_p, ctypes.POINTER(_PageTableArgs), ctypes.c_void_p]
+_lib.lumo_pages_compact.argtypes = [ctypes.c_void_p, ctypes.POINTER(_PageTableArgs), ctypes.c_void_p]
+for _f in (_lib.lumo_pages_fork, _lib.lumo_pages_free):
+    _f.argtypes = [ctypes.c_void_p, ctypes.POINTER(_PageTableArgs), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
+_lib.lumo_pages_reserve.argtypes = [ctypes.c_void_p, ctypes.POINTER(_PageTableArgs), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                    ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
+_lib.lumo_rows_copy.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
+
 _ACCEPT_MODES = {"greedy": 0, "rejection": 1}
 _SELECT_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -146,6 +202,32 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("tensors passed to the library must be contiguous CUDA tensors")
     return t.data_ptr()
+
+
+def _rows_ptr(t: Optional[torch.Tensor], heads: int, dh: int, name: str):
+    """Pointer and token stride of a tensor [..., heads, dh] whose heads are adjacent and whose tokens may be parts of longer rows."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.shape[-2:] != (heads, dh) or t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != dh):
+        raise ValueError(f"{name} must be a CUDA tensor [..., {heads}, {dh}] with adjacent heads")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    stride = t.stride(-3)
+    for i in range(t.dim() - 3):
+        if t.shape[i] != 1 and t.stride(i) != stride * int(np.prod(t.shape[i + 1:-2])):
+            raise ValueError(f"{name}: the tokens must be evenly spaced")
+    return t.data_ptr(), stride
+
+
+def _int32(**tensors):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError(f"{name} must be int32")
+
+
+def pages_work_ints(n_rows: int, n_pages: int) -> int:
+    """Ints of scratch a page table's calls need."""
+    return int(_lib.lumo_pages_work_ints(int(n_rows), int(n_pages)))
 
 
 _cuda_ready = torch.cuda.is_initialized
@@ -300,6 +382,81 @@ class Context:
         self._check(_lib.lumo_kv_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length),
                                          int(accepted.shape[1]), _ptr(ctx_len_out), _stream(stream)))
 
+    # ---- norm and rotation, the paged 4-bit cache ----
+    def qk_norm_rope(self, layer: "QkNormRope", desc: Optional["TreeDesc"] = None, stream=None):
+        """Norm of every query and key head and the position rotation, in one pass; with ``desc`` the tokens are its trees' nodes."""
+        self._check(_lib.lumo_qk_norm_rope(self._h, desc._h if desc is not None else None, layer.args, _stream(stream)))
+
+    @staticmethod
+    def pack_kv4(layers: Sequence["Kv4Layer"]):
+        return (_Kv4Args * len(layers))(*[l.args for l in layers])
+
+    def kv4_work_bytes(self, desc: "TreeDesc", Hq: int, Hkv: int, n_splits: int = 0) -> int:
+        """Bytes of workspace ``kv4_attention`` needs (Kv4Layer's ``work``)."""
+        return int(_lib.lumo_kv4_work_bytes(self._h, desc._h, int(Hq), int(Hkv), int(n_splits)))
+
+    def kv4_write_tree(self, desc: "TreeDesc", layers, stream=None):
+        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        self._check(_lib.lumo_kv4_write_tree(self._h, desc._h, arr, len(arr), _stream(stream)))
+
+    def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, stream=None):
+        """Entries of listed tokens (int32 rows and positions, [T]); a layer's ``status`` then has a word per token."""
+        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        _int32(tok_row=tok_row, tok_pos=tok_pos)
+        self._check(_lib.lumo_kv4_append(self._h, arr, len(arr), tok_row.numel(), _ptr(tok_row), _ptr(tok_pos), _stream(stream)))
+
+    def kv4_read(self, layer: "Kv4Layer", tok_row: torch.Tensor, tok_pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, stream=None):
+        """The listed tokens' entries as bf16 [T, Hkv, dh]."""
+        _int32(tok_row=tok_row, tok_pos=tok_pos)
+        self._check(_lib.lumo_kv4_read(self._h, layer.args, tok_row.numel(), _ptr(tok_row), _ptr(tok_pos), _ptr(k_out), _ptr(v_out),
+                                       _stream(stream)))
+
+    def kv4_attention(self, desc: "TreeDesc", layers, stream=None):
+        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        self._check(_lib.lumo_kv4_attention(self._h, desc._h, arr, len(arr), _stream(stream)))
+
+    def kv4_publish(self, desc: "TreeDesc", layers, accepted: torch.Tensor, length: torch.Tensor,
+                    ctx_len_out: Optional[torch.Tensor] = None, stream=None):
+        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), int(accepted.shape[1]),
+                                          _ptr(ctx_len_out), _stream(stream)))
+
+    # ---- pages ----
+    def pages_init(self, table: "PageTable", stream=None):
+        self._check(_lib.lumo_pages_init(self._h, table.args, _stream(stream)))
+
+    def pages_fork(self, table: "PageTable", src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
+        """Row dst[i], empty so far, shares the pages of row src[i]."""
+        _int32(src=src, dst=dst, status=status)
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst must have the same length")
+        self._check(_lib.lumo_pages_fork(self._h, table.args, _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream(stream)))
+
+    def pages_reserve(self, table: "PageTable", rows: torch.Tensor, start: torch.Tensor, end: Optional[torch.Tensor] = None, add: int = 0,
+                      status: Optional[torch.Tensor] = None, stream=None):
+        """Positions [start, end) (or [start, start + add)) of the rows made writable: shared pages copied, missing ones added."""
+        _int32(rows=rows, start=start, end=end, status=status)
+        self._check(_lib.lumo_pages_reserve(self._h, table.args, _ptr(rows), _ptr(start), _ptr(end), int(add), rows.numel(), _ptr(status),
+                                            _stream(stream)))
+
+    def pages_free(self, table: "PageTable", rows: torch.Tensor, keep: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                   stream=None):
+        """Pages behind the rows' first ``keep`` positions (all pages without it) given back."""
+        _int32(rows=rows, keep=keep, status=status)
+        self._check(_lib.lumo_pages_free(self._h, table.args, _ptr(rows), _ptr(keep), rows.numel(), _ptr(status), _stream(stream)))
+
+    def pages_compact(self, table: "PageTable", stream=None):
+        """The pages in use moved to the lowest numbers, in all pools and tables."""
+        self._check(_lib.lumo_pages_compact(self._h, table.args, _stream(stream)))
+
+    def rows_copy(self, blocks: "RowBlocks", src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
+        """Row src[i] of every block copied to its row dst[i]."""
+        _int32(src=src, dst=dst, status=status)
+        if src.numel() != dst.numel():
+            raise ValueError("src and dst must have the same length")
+        self._check(_lib.lumo_rows_copy(self._h, blocks.ptrs, blocks.row_bytes, len(blocks.tensors), blocks.n_rows, _ptr(src), _ptr(dst),
+                                        src.numel(), _ptr(status), _stream(stream)))
+
 
 class TreeDesc:
     """lumo_tree_desc built from host arrays parent [B, N] (and optional slot, depth)."""
@@ -418,3 +575,118 @@ class AttnLayer:
         for name in self.tensors:
             setattr(a, name, _ptr(self.tensors[name]))
         self.args = a
+
+
+class QkNormRope:
+    """lumo_qk_args: the norm and rotation in front of one full-attention layer; keeps the tensors alive."""
+
+    def __init__(self, *, q, q_out, k=None, k_out=None, inv_freq=None, q_weight=None, k_weight=None, normalise: bool = True, eps: float = 1e-6,
+                 weight_offset: float = 0.0, mscale: float = 1.0, style: str = "half", pos=None, ctx_len=None, sections=None, turns: bool = False):
+        """q [..., Hq, dh], k [..., Hkv, dh] (tokens may be parts of longer rows), outputs alike; inv_freq [rot / 2] fp32.  pos: int32 [T], or
+        [3, T] with ``sections``, the pairs of each axis, in blocks or (``turns``) taking turns; without pos the call's trees give the
+        positions, behind ctx_len [B].  style: "half" or "pairs"."""
+        self.tensors = dict(q=q, k=k, q_out=q_out, k_out=k_out, inv_freq=inv_freq, q_weight=q_weight, k_weight=k_weight, pos=pos, ctx_len=ctx_len)
+        for name in ("k", "q_out", "k_out", "q_weight", "k_weight"):
+            t = self.tensors[name]
+            if t is not None and t.dtype != q.dtype:
+                raise ValueError(f"{name} must have the dtype of q")
+        if inv_freq is not None and inv_freq.dtype != torch.float32:
+            raise ValueError("inv_freq must be float32")
+        _int32(pos=pos, ctx_len=ctx_len)
+        Hq, dh = int(q.shape[-2]), int(q.shape[-1])
+        Hkv = int(k.shape[-2]) if k is not None else 0
+        a = _QkArgs()
+        a.T, a.Hq, a.Hkv, a.dh, a.dtype = q.numel() // (Hq * dh), Hq, Hkv, dh, _DTYPE[q.dtype]
+        if (k is None) != (k_out is None) or q_out.shape != q.shape or (k is not None and (k_out.shape != k.shape or k.numel() != a.T * Hkv * dh)):
+            raise ValueError("outputs must have their inputs' shapes, and q and k the same tokens")
+        a.rot = 2 * int(inv_freq.numel()) if inv_freq is not None else 0
+        a.style, a.turns = {"half": 0, "pairs": 1}[style], int(turns)
+        a.axes = 3 if sections is not None else 1
+        if sections is not None:
+            a.section[:] = [int(v) for v in sections]
+        if pos is not None and pos.numel() != a.axes * a.T:
+            raise ValueError("pos must have a number per axis and token")
+        for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if t is not None and t.numel() != dh:
+                raise ValueError(f"{name} must have dh elements")
+        a.normalise, a.eps, a.weight_offset, a.mscale = int(normalise), float(eps), float(weight_offset), float(mscale)
+        for name, heads in (("q", Hq), ("k", Hkv), ("q_out", Hq), ("k_out", Hkv)):
+            ptr, stride = _rows_ptr(self.tensors[name], heads, dh, name)
+            setattr(a, name, ptr)
+            setattr(a, name + "_stride", stride)
+        for name in ("q_weight", "k_weight", "inv_freq", "pos", "ctx_len"):
+            setattr(a, name, _ptr(self.tensors[name]))
+        self.args = a
+
+
+class Kv4Layer:
+    """lumo_kv4_args for one full-attention layer over a paged 4-bit cache; keeps the tensors alive."""
+
+    def __init__(self, *, Hq: int, Hkv: int, pages, table, page_size: int, scale: float = 1.0, ctx_len=None, cache_row=None, refs=None, q=None,
+                 k_new=None, v_new=None, out=None, lse=None, k_exp: int = 0, v_exp: int = 0, n_splits: int = 0, status=None, work=None):
+        """pages: uint8 [n_pages, Hkv, 2, page_size * 72]; table: int32 [rows, max_pages]."""
+        self.tensors = dict(pages=pages, table=table, refs=refs, ctx_len=ctx_len, cache_row=cache_row, q=q, k_new=k_new, v_new=v_new, out=out,
+                            lse=lse, status=status, work=work)
+        if pages.dtype != torch.uint8 or pages.dim() != 4 or tuple(pages.shape[1:]) != (Hkv, 2, page_size * 72):
+            raise ValueError("pages must be a uint8 tensor [n_pages, Hkv, 2, page_size * 72]")
+        if table.dim() != 2:
+            raise ValueError("table must be [rows, max_pages]")
+        _int32(table=table, refs=refs, ctx_len=ctx_len, cache_row=cache_row, status=status)
+        for name in ("q", "k_new", "v_new"):
+            t = self.tensors[name]
+            if t is not None and t.dtype != torch.bfloat16:
+                raise ValueError(f"{name} must be bfloat16")
+        if lse is not None and lse.dtype != torch.float32:
+            raise ValueError("lse must be float32")
+        a = _Kv4Args()
+        a.Hq, a.Hkv, a.dh, a.scale = int(Hq), int(Hkv), 128, float(scale)
+        a.n_rows, a.max_pages = int(table.shape[0]), int(table.shape[1])
+        a.n_pages, a.page_size = int(pages.shape[0]), int(page_size)
+        a.k_exp, a.v_exp, a.n_splits = int(k_exp), int(v_exp), int(n_splits)
+        a.out_dtype = _DTYPE[out.dtype] if out is not None else LUMO_F32
+        a.q, a.q_stride = _rows_ptr(q, int(Hq), 128, "q")
+        a.k_new, a.kv_stride = _rows_ptr(k_new, int(Hkv), 128, "k_new")
+        a.v_new, v_stride = _rows_ptr(v_new, int(Hkv), 128, "v_new")
+        if k_new is not None and v_new is not None and v_stride != a.kv_stride:
+            raise ValueError("k_new and v_new must have the same token stride")
+        for name in ("pages", "table", "refs", "ctx_len", "cache_row", "out", "lse", "status", "work"):
+            setattr(a, name, _ptr(self.tensors[name]))
+        a.work_bytes = work.numel() * work.element_size() if work is not None else 0
+        self.args = a
+
+
+class PageTable:
+    """lumo_page_table: pages of a cache (any kind), the rows that hold them and the free ones; keeps the tensors alive."""
+
+    def __init__(self, *, page_size: int, table, row_pages, refs, free_list, free_count, work, pools=()):
+        """table int32 [rows, max_pages], row_pages int32 [rows], refs and free_list int32 [n_pages], free_count int32 [1], work int32
+        [pages_work_ints(rows, n_pages)]; pools: tensors [n_pages, ...] of equal page sizes."""
+        self.tensors = dict(table=table, row_pages=row_pages, refs=refs, free_list=free_list, free_count=free_count, work=work)
+        self.pools = list(pools)
+        _int32(**self.tensors)
+        n_rows, max_pages, n_pages = int(table.shape[0]), int(table.shape[1]), int(refs.numel())
+        if row_pages.numel() != n_rows or free_list.numel() != n_pages or free_count.numel() != 1 or work.numel() < pages_work_ints(n_rows, n_pages):
+            raise ValueError("row_pages, free_list, free_count or work does not fit table and refs")
+        sizes = {t.numel() // n_pages * t.element_size() for t in self.pools}
+        if any(t.shape[0] != n_pages for t in self.pools) or len(sizes) > 1:
+            raise ValueError("pools must be [n_pages, ...] with pages of one size")
+        self._ptrs = (ctypes.c_void_p * max(1, len(self.pools)))(*[_ptr(t) for t in self.pools])
+        a = _PageTableArgs()
+        a.n_rows, a.max_pages, a.n_pages, a.page_size = n_rows, max_pages, n_pages, int(page_size)
+        for name, t in self.tensors.items():
+            setattr(a, name, _ptr(t))
+        a.n_pools, a.pools = len(self.pools), ctypes.addressof(self._ptrs)
+        a.page_bytes = sizes.pop() if sizes else 16
+        self.args = a
+
+
+class RowBlocks:
+    """Tensors [n_rows, ...] whose rows ``Context.rows_copy`` copies (recurrent states, convolution histories); keeps them alive."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.n_rows = int(self.tensors[0].shape[0])
+        if any(t.shape[0] != self.n_rows for t in self.tensors):
+            raise ValueError("the blocks must have the same number of rows")
+        self.ptrs = (ctypes.c_void_p * len(self.tensors))(*[_ptr(t) for t in self.tensors])
+        self.row_bytes = (ctypes.c_int64 * len(self.tensors))(*[t.numel() // self.n_rows * t.element_size() for t in self.tensors])

@@ -365,6 +365,91 @@ cudaError_t launch_commit(const Shape& s, const TreeDev& t, const LayerBatch& lb
 cudaError_t launch_path_from_node(const TreeDev& t, int B, int N, const int32_t* node, int lmax,
                                   int32_t* accepted, int32_t* len, int32_t* status, bool pdl, cudaStream_t st);
 
+// ---- norm and rotation of queries and keys (rope.cu) ---------------------------------------
+struct RopeArgs {
+  const void* q; const void* k; void* q_out; void* k_out;
+  long long q_stride, k_stride, q_out_stride, k_out_stride;   // elements from token to token
+  int T, Hq, Hkv, dh, rot, style, norm, axes, turns;
+  int section[3];
+  const float* inv_freq;
+  const int32_t* pos;                                 // [axes, T], or null: ctx_len[t / N] + depth[t] - 1
+  const int32_t* ctx_len; const int32_t* depth; int N;
+  const void* q_weight; const void* k_weight;
+  float eps, weight_offset, mscale;
+};
+cudaError_t launch_rope(const RopeArgs& a, int dtype, int sms, bool pdl, cudaStream_t st);
+
+// ---- the paged 4-bit cache (kv4_io.cu, kv4_attn.cu) -----------------------------------------
+constexpr int kKv4Entry = 72;                         // bytes of one position's keys (or values) of a head: 64 of codes, 8 of scales
+struct Kv4Shape {
+  int B, N, Ns, Hq, Hkv, n_rows, max_pages, n_pages, page, page_log2;
+  int k_exp, v_exp;
+  const int32_t* table; const int32_t* refs;
+  const int32_t* ctx_len; const int32_t* cache_row;
+  const int32_t* parent; const int32_t* slot;
+  long long kv_stride;                                // elements from token to token in k_new and v_new
+};
+template <int CAP>
+struct Kv4LayersT {
+  void* pages[CAP];
+  const void* kn[CAP]; const void* vn[CAP];
+  int32_t* status[CAP];
+};
+using Kv4Layers = Kv4LayersT<kMaxAttnLayers>;
+using FewKv4Layers = Kv4LayersT<kFewLayers>;
+inline FewKv4Layers few_layers(const Kv4Layers& L) {
+  FewKv4Layers f;
+  for (int i = 0; i < kFewLayers; ++i) { f.pages[i] = L.pages[i]; f.kn[i] = L.kn[i]; f.vn[i] = L.vn[i]; f.status[i] = L.status[i]; }
+  return f;
+}
+// tokens listed one by one: T of them, rows and positions on the device
+struct Kv4Tokens { int T; const int32_t* row; const int32_t* pos; };
+cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_kv4_append(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const Kv4Tokens& t, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int32_t* status, int sms,
+                            bool pdl, cudaStream_t st);
+cudaError_t launch_kv4_publish(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const int32_t* accepted, const int32_t* len, int lmax,
+                               int32_t* ctx_len_out, bool pdl, cudaStream_t st);
+
+struct Kv4AttnPtrs { const void* pages; const void* q; void* out; float* lse; int32_t* status; };
+struct Kv4AttnArgs {
+  const unsigned char* pages; const void* q; void* out; float* lse; int32_t* status;
+  float* part_o; float* part_lse; int32_t* cta_code; int2* unit_slots;
+  const int32_t* ctx_len; const int32_t* cache_row; const int32_t* table;
+  const uint32_t* vis; const uint32_t* used;
+  long long q_stride;
+  int B, N, Ns, Hq, Hkv, G, RT, R, n_rows, max_pages, n_pages, page_log2, max_pos;   // RT row tiles of R rows each
+  int S;                                              // partitions per unit; 0: the CTAs share the list of tiles evenly
+  int C;                                              // CTAs of the attention launch
+  int out_bf16;
+  float scale_log2;                                   // scale * log2(e) * 2^k_exp
+  float v_mul;                                        // 2^v_exp
+};
+struct Kv4Plan { Kv4AttnArgs a; int kind; };           // kind: 0 register form, 1 tensor memory form
+size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms);
+void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
+              int n_splits, void* work, int sms, Kv4Plan* plan);
+cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st);
+cudaError_t launch_kv4_merge(const Kv4Plan& plan, bool pdl, cudaStream_t st);
+
+// ---- page tables (pages.cu) -----------------------------------------------------------------
+constexpr int kMaxPools = 64;
+constexpr int kMaxPageRows = 1024;                    // rows one page call lists
+constexpr int kMaxPages = 1 << 18;                    // pages of a table
+struct PagePools { unsigned char* p[kMaxPools]; long long bytes[kMaxPools]; int n; };
+struct PageTableDev {
+  int n_rows, max_pages, n_pages, page;
+  int32_t* table; int32_t* row_pages; int32_t* refs; int32_t* free_list; int32_t* free_count; int32_t* work;
+};
+cudaError_t launch_pages_init(const PageTableDev& t, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_pages_fork(const PageTableDev& t, const int32_t* src, const int32_t* dst, int n, int32_t* status, bool pdl, cudaStream_t st);
+cudaError_t launch_pages_free(const PageTableDev& t, const int32_t* rows, const int32_t* keep, int n, int32_t* status, bool pdl, cudaStream_t st);
+cudaError_t launch_pages_reserve(const PageTableDev& t, const PagePools& pools, const int32_t* rows, const int32_t* start, const int32_t* end,
+                                 int add, int n, int32_t* status, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_pages_compact(const PageTableDev& t, const PagePools& pools, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_rows_copy(const PagePools& blocks, int n_rows, const int32_t* src, const int32_t* dst, int n, int32_t* status, int sms,
+                             bool pdl, cudaStream_t st);
+
 // ---- attention half (attn.cu) ------------------------------------------------------------
 struct AttnShape {
   int B, N, Ns, Hq, Hkv, S, n_rows, max_pos, layout;

@@ -1,0 +1,719 @@
+// Ancestry-masked decode attention over the paged 4-bit cache (sm_100a):
+//
+//   out[b,i,h,:] = sum_p softmax_p(scale q[b,i,h] . k[p]) v[p]  over the context and the node's ancestors and itself
+//
+// Keys and values come as e2m1 codes and e4m3 scales, 144 bytes a position and KV head.  A code times its scale has at most six
+// significant bits, so it is exact in f16: the tensor cores multiply f16 operands whose only roundings are those of the
+// probabilities (2^-12 relative each).  A query row is scaled by a power of two to fit f16 (its elements are bf16: eight bits) and the logits
+// are scaled back in fp32; sums are fp32.
+//
+// The work is the list of 128-key tiles of all (sequence, KV head, row tile) units in order; a CTA takes a contiguous share of the list, and
+// every piece of its share that lies in one unit is a SEGMENT, whose normalised output and base-2 log-sum-exp go to a slot;
+// kv4_merge_kernel combines the slots of a unit in key order.  A tile is staged by bulk copies, one per page: a head's keys and values
+// of a page are adjacent.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "internal.h"
+#include "kv4.h"
+
+namespace lumo {
+
+namespace {
+
+constexpr int kDh = 128;
+constexpr int kKeys = 128;            // keys per tile
+constexpr int kTileBytes = kKeys * 2 * kKv4Entry;   // 18432: keys and values, codes and scales
+constexpr int kSeqCache = 64;         // sequences whose context length, cache row and tile count are kept in shared memory
+constexpr float kLag = 8.f;           // the reference maximum moves when exceeded by more than this (log2 units)
+constexpr float kLift = 6.f;          // probabilities are held as 2^kLift times themselves: at most 2^14 in f16, and what f16 drops is below 2^-30
+constexpr uint32_t kSpinLimit = 1u << 24;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory");
+}
+// Bounded wait: false if the phase did not complete within the spin limit.
+__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity) {
+  const uint32_t addr = smem_u32(bar);
+  for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+// untiled bulk copy into shared memory: both addresses 16-byte aligned, a multiple of 16 bytes; completion counted on `bar`
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, unsigned long long* bar, uint64_t policy) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;\n"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint64_t l2_evict_first_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// (base-2 log-sum-exp of a row from its reference maximum and lifted sum; a NaN stays one, a row without keys gives -inf)
+__device__ __forceinline__ float row_lse2(float m, float l) { return l == 0.f ? -INFINITY : m - kLift + log2f(l); }
+__device__ __forceinline__ float row_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// The power of two that takes a query row to f16: its largest magnitude becomes 2^14 to 2^15.  `top`: that magnitude's bits.
+__device__ __forceinline__ int query_exponent(uint32_t top) {
+  const int e = (int)(top >> 23) - 127;
+  return min(14 - e, 120);
+}
+
+// ---- work decomposition ----------------------------------------------------------------
+// Units are numbered u = (b * Hkv + hkv) * RT + rt; unit u owns nt(b) tiles (0 for a sequence that fails its check).  Automatic mode: the
+// units are laid end to end on a line, each preceded by `cost` idle positions (the price of starting it, in tiles); CTA c owns the
+// positions [c * per, (c + 1) * per), works on the tiles among them, and the slot of a segment is u + c (strictly increasing along the line,
+// so unique).  Fixed mode (S partitions): CTA c owns partition c mod S of unit c / S, slot c.
+struct SeqCache { int ctx[kSeqCache], row[kSeqCache], nt[kSeqCache]; };
+struct Segment {
+  int b, hkv, rt;     // unit
+  int t0, n;          // first tile within the unit, tile count (n = 0 possible in fixed mode)
+  int slot;
+  int unit, slot0, nslots;   // the unit, and the slots all its segments write (ascending along the key range)
+  int ctx, crow;
+};
+
+__device__ __forceinline__ int seq_tiles(const Kv4AttnArgs& a, int cx, int cr) {
+  return seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos) == LUMO_SEQ_OK ? (cx + a.Ns + kKeys - 1) / kKeys : 0;
+}
+__device__ __forceinline__ void fill_seq_cache(const Kv4AttnArgs& a, SeqCache& s) {
+  if (threadIdx.x < kSeqCache && threadIdx.x < a.B) {
+    const int cx = a.ctx_len[threadIdx.x], cr = a.cache_row[threadIdx.x];
+    s.ctx[threadIdx.x] = cx; s.row[threadIdx.x] = cr; s.nt[threadIdx.x] = seq_tiles(a, cx, cr);
+  }
+}
+
+template <int kCost, int kMinTiles, int kSlack>
+struct Work {
+  const Kv4AttnArgs& a;
+  const SeqCache& sc;
+  int b = 0, q = 0;   // current sequence, unit within the sequence
+  int g = 0, g_end = 0;       // next position on the line, end of this CTA's share (the host bounds the line below 2^31)
+  int g_unit = 0;     // position at which the current unit's stretch (idle prefix, then its tiles) starts
+  int nt = 0;         // tiles per unit of the current sequence
+  int per = 1;        // automatic mode: positions per CTA
+  int parts;          // partitions per unit when CTA c owns partition c mod parts of unit c / parts; 0: shares of the line
+  bool fixed_done = false;
+
+  __device__ __forceinline__ int tiles_of(int bb, int* ctx, int* crow) const {
+    if (bb < kSeqCache) { *ctx = sc.ctx[bb]; *crow = sc.row[bb]; return sc.nt[bb]; }
+    *ctx = a.ctx_len[bb];
+    *crow = a.cache_row[bb];
+    return seq_tiles(a, *ctx, *crow);
+  }
+
+  __device__ Work(const Kv4AttnArgs& args, const SeqCache& cache) : a(args), sc(cache), parts(args.S) {
+    if (parts > 0) return;
+    const int upb = a.Hkv * a.RT;       // units per sequence
+    int total = 0, most = 0, cx, cr;
+    for (int bb = 0; bb < a.B; ++bb) {
+      const int n = tiles_of(bb, &cx, &cr);
+      if (n > 0) total += (n + kCost) * upb;
+      most = max(most, n);
+    }
+    per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+    // Short contexts: when there is a CTA for every unit and no unit is much longer than an even share, units stay whole: nothing
+    // is cut, and with one segment per unit the outputs are final when they leave this kernel.
+    if (a.B * upb <= (int)gridDim.x && most <= per + kSlack) { parts = 1; return; }
+    if (per < kMinTiles) per = kMinTiles;
+    g = (int)blockIdx.x * per;
+    g_end = g + per < total ? g + per : total;
+    int acc = 0;                        // the unit whose stretch holds position g
+    for (b = 0; b < a.B; ++b) {
+      nt = tiles_of(b, &cx, &cr);
+      const int span = nt > 0 ? (nt + kCost) * upb : 0;
+      if (g < acc + span) { q = (g - acc) / (nt + kCost); g_unit = acc + q * (nt + kCost); break; }
+      acc += span;
+    }
+  }
+
+  // next segment of this CTA; false when the share is exhausted
+  __device__ __forceinline__ bool next(Segment* s) {
+    const int upb = a.Hkv * a.RT;
+    if (parts > 0) {
+      if (fixed_done) return false;
+      fixed_done = true;
+      const int u = blockIdx.x / parts, part = blockIdx.x - u * parts;
+      s->b = u / upb;
+      if (s->b >= a.B) return false;
+      const int r = u - s->b * upb;
+      s->hkv = r / a.RT; s->rt = r - s->hkv * a.RT;
+      const int n_all = tiles_of(s->b, &s->ctx, &s->crow);
+      s->t0 = (int)(((long long)part * n_all) / parts);
+      s->n = (int)(((long long)(part + 1) * n_all) / parts) - s->t0;
+      s->slot = blockIdx.x;
+      s->unit = u; s->slot0 = u * parts; s->nslots = parts;
+      return n_all > 0;
+    }
+    while (g < g_end && b < a.B) {
+      if (nt == 0 || g >= g_unit + nt + kCost) {         // move to the next unit (skipping sequences without tiles)
+        if (nt > 0) g_unit += nt + kCost;
+        if (nt == 0 || ++q == upb) {
+          q = 0;
+          int cx, cr;
+          do { ++b; nt = b < a.B ? tiles_of(b, &cx, &cr) : 0; } while (b < a.B && nt == 0);
+        }
+        continue;
+      }
+      const int first = g_unit + kCost;                  // position of the unit's tile 0
+      const int lo = g > first ? g : first;
+      const int hi = first + nt < g_end ? first + nt : g_end;
+      g = g_unit + nt + kCost < g_end ? g_unit + nt + kCost : g_end;
+      if (lo >= hi) continue;                            // only idle positions of this unit fall into the share
+      const int u = b * upb + q;
+      s->b = b; s->hkv = q / a.RT; s->rt = q - s->hkv * a.RT;
+      tiles_of(b, &s->ctx, &s->crow);
+      s->t0 = lo - first;
+      s->n = hi - lo;
+      s->slot = u + blockIdx.x;
+      s->unit = u;
+      s->slot0 = u + first / per;
+      s->nslots = (first + nt - 1) / per - first / per + 1;
+      return true;
+    }
+    return false;
+  }
+};
+
+// Stages one tile: a bulk copy per page that holds positions below ctx + Ns (the lanes of the loading warp take a page each).  A page
+// number out of range sets *bad_page, and nothing is copied for it.
+__device__ __forceinline__ void load_tile(const Kv4AttnArgs& a, const Segment& sg, int tile, uint32_t dst, unsigned long long* full, uint32_t* bad_page,
+                                          uint64_t policy) {
+  const int lane = threadIdx.x & 31;
+  const int page = 1 << a.page_log2, per_tile = kKeys >> a.page_log2;
+  const int pos = tile * kKeys + (lane << a.page_log2);
+  const bool mine = lane < per_tile && pos < sg.ctx + a.Ns;
+  int pg = -1;
+  if (mine) pg = __ldg(a.table + (size_t)sg.crow * a.max_pages + (pos >> a.page_log2));
+  const bool ok = mine && pg >= 0 && pg < a.n_pages;
+  const uint32_t bytes = page * 2 * kKv4Entry;
+  const unsigned good = __ballot_sync(0xffffffffu, ok);
+  const bool bad = __any_sync(0xffffffffu, mine && !ok);
+  if (lane == 0) {
+    if (bad) *reinterpret_cast<volatile uint32_t*>(bad_page) = 1;
+    mbar_expect_tx(full, __popc(good) * bytes);
+  }
+  __syncwarp();
+  if (ok) bulk_load(dst + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, 0), bytes, full, policy);
+}
+
+__device__ __forceinline__ bool slot_seen(const uint32_t* row, int s) {        // s: suffix slot; below 0: context
+  return s < 0 || (s < kMaxAttnSlots && ((__ldg(row + (s >> 5)) >> (s & 31)) & 1u));
+}
+
+// ---- register form -----------------------------------------------------------------------
+// For up to 8 NT query rows per unit (a token or a short tree of one request times its head group).  Bound by the cache's bytes, so the point is
+// to keep them coming and to spend few instructions on each: one warp issues the bulk copies into a ring of eight tiles, and the others turn
+// codes into matrix operands in registers, without a second trip through shared memory.  A warp takes 16 keys of a tile:
+//
+//   S^T [16 keys x 8 rows] = K Q^T, eight m16n8k16 products; lane (g, t) of a warp (g = lane / 4, t = lane % 4) supplies elements
+//       [32 t, 32 t + 32) of two keys, one 16-byte read each: which element stands at which place of the inner dimension is free as long as
+//       Q's fragments agree
+//   O^T [128 x 8 rows] += V^T P^T, eight products (one per 16 elements of the head): lane (g, t) supplies block g of four keys.  The two
+//       codes of a byte have to belong to two keys: the nibbles of two keys' words are interleaved (two instructions per eight codes).
+//       P^T comes out of S^T's accumulators by an 8 x 8 transposition across the warp.
+//
+// Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
+// The instruction count (about 420 per 16 keys and warp, of which 320 turn codes into f16) is near the time the bytes take.
+template <int NT> struct Small {
+  static constexpr int kWarps = NT == 1 ? 16 : 8;        // consumers; NT = 2 needs twice the registers
+  static constexpr int kStages = 8;
+  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kRedRow = 132;                    // floats per row of the reduction buffer: the stores of a half warp meet no bank twice
+  static constexpr int kOffRed = kStages * kTileBytes;
+  static constexpr int kOffCtl = kOffRed + kWarps * 8 * kRedRow * 4;
+  struct Ctl {
+    unsigned long long full[kStages], empty[kStages];
+    SeqCache seq;
+    float stat[kWarps][8 * NT][2];                       // a warp's reference maximum and sum of each row
+    uint32_t timed_out;
+    uint32_t bad_page[16];                               // by segment number mod 16: the loader is never that far ahead
+  };
+  static constexpr int kBytes = kOffCtl + (int)sizeof(Ctl);
+  using W = Work<5, 2, 3>;
+};
+static_assert(Small<1>::kBytes <= 227 * 1024 && Small<2>::kBytes <= 227 * 1024, "one CTA per SM");
+
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
+  return r;
+}
+
+template <int NT>
+__global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(const Kv4AttnArgs a) {
+  using C = Small<NT>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  typename C::Ctl& sm = *reinterpret_cast<typename C::Ctl*>(smem + C::kOffCtl);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 8); }
+    sm.timed_out = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (tid < 16) sm.bad_page[tid] = 0;
+  pdl_wait();          // everything below may belong to earlier kernels
+  pdl_trigger();
+  fill_seq_cache(a, sm.seq);
+  __syncthreads();
+  typename C::W work(a, sm.seq);
+  Segment sg;
+  bool ok = true;
+  uint32_t it = 0;     // tiles of this CTA so far, over all segments
+  uint32_t nseg = 0;
+
+  if (warp == C::kWarps) {
+    // ---------------- loader ----------------
+    const uint64_t policy = l2_evict_first_policy();
+    while (work.next(&sg)) {
+      for (int j = 0; j < sg.n; ++j, ++it) {
+        const uint32_t st = it % C::kStages, use = it / C::kStages;
+        if (use > 0 && ok) ok = mbar_wait(&sm.empty[st], (use - 1) & 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (j == 0 && lane == 0) sm.bad_page[nseg & 15u] = 0;
+        load_tile(a, sg, sg.t0 + j, smem_u32(smem) + st * kTileBytes, &sm.full[st], &sm.bad_page[nseg & 15u], policy);
+      }
+      if (!ok) break;
+      if (sg.n > 0) ++nseg;
+    }
+    if (!ok && lane == 0) sm.timed_out = 1;
+    // no copy may be on its way when the CTA leaves: the last use of every stage (complete already unless a wait ran out)
+    for (uint32_t s = 0; s < C::kStages && s < it; ++s) mbar_wait(&sm.full[s], (((it - 1 - s) / C::kStages)) & 1u);
+  } else {
+    // ---------------- consumers ----------------
+    const int g = lane >> 2, t = lane & 3;
+    const int grp = warp & 7;                            // keys [16 grp, 16 grp + 16) of a tile
+    const int GN = a.G * a.N, page = 1 << a.page_log2;
+    const int c0 = grp * 16, pi = c0 >> a.page_log2, r0 = c0 & (page - 1);      // the group's page in the tile, first position in it
+    const int kq = (g >> 1) + (g & 1) * 4;               // position of matrix row g among eight keys: lane t's value keys are t and t + 4
+    const uint32_t page_off = pi * page * 2 * kKv4Entry;
+    const uint32_t k_codes = page_off + (r0 + kq) * 64 + t * 16, k_scales = page_off + page * 64 + (r0 + kq) * 8 + t * 2;
+    const uint32_t v_codes = page_off + page * kKv4Entry + (r0 + t) * 64 + g * 8;
+    const uint32_t v_scales = page_off + page * (kKv4Entry + 64) + (r0 + t) * 8 + g;
+    float* red = reinterpret_cast<float*>(smem + C::kOffRed);
+    while (work.next(&sg)) {
+      if (tid == 0) a.unit_slots[sg.unit] = make_int2(sg.slot0, sg.nslots);   // for the merge (same pair from every writer)
+      // query fragments: row 8 nt + g, elements [32 t, 32 t + 32)
+      uint32_t qf[NT][16];
+      float mul[NT][2];                                  // logits of rows 8 nt + 2 t, + 1 back from the scaled queries, in log2 units
+      const uint32_t* vis[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = sg.rt * a.R + nt * 8 + g;
+        const bool in = r < GN;
+        const int hl = in ? r / a.N : 0, node = in ? r - hl * a.N : 0;
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)sg.b * a.N + node) * a.q_stride +
+                                                          ((size_t)sg.hkv * a.G + hl) * kDh + t * 32);
+        uint32_t w[16], top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 v = in ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+          w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max(top, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = query_exponent(top);
+        const float up = exp2i(e);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) qf[nt][i] = pack_half2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xFFFF0000u) * up);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int lr = 2 * t + h;                      // the accumulators' row
+          mul[nt][h] = a.scale_log2 * exp2i(-__shfl_sync(0xffffffffu, e, lr * 4));
+          const int rr = sg.rt * a.R + nt * 8 + lr;
+          vis[nt][h] = a.vis + ((size_t)sg.b * a.N + (rr < GN ? rr % a.N : 0)) * 8;
+        }
+      }
+      const uint32_t* usedw = a.used + (size_t)sg.b * 8;
+      float o[NT][8][4], m[NT][2], l[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.f;
+        m[nt][0] = m[nt][1] = -INFINITY;
+        l[nt][0] = l[nt][1] = 0.f;
+      }
+      for (int j = 0; j < sg.n; ++j, ++it) {
+        if (C::kWarps == 16 && (int)(it & 1u) != warp >> 3) continue;           // the other eight warps' tile
+        const uint32_t st = it % C::kStages;
+        if (ok) ok = mbar_wait(&sm.full[st], (it / C::kStages) & 1u);
+        const int pos0 = (sg.t0 + j) * kKeys + c0;       // the group's first position
+        if (ok && pos0 < sg.ctx + a.Ns) {
+          const unsigned char* tile = smem + st * kTileBytes;
+          const bool tail = pos0 + 16 > sg.ctx;
+          // ---- S^T
+          float s[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+          {
+            const uint4 ka = *reinterpret_cast<const uint4*>(tile + k_codes), kb = *reinterpret_cast<const uint4*>(tile + k_codes + 8 * 64);
+            const uint32_t sa = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(tile + k_scales));
+            const uint32_t sb = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(tile + k_scales + 8 * 8));
+            const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {                // 32 t + 8 w ..: block 2 t for w < 2
+              uint32_t ha[4], hb[4];
+              e2m1x8_to_half2(wa[w], ha);
+              e2m1x8_to_half2(wb[w], hb);
+              const uint32_t fa = __byte_perm(sa, 0, w < 2 ? 0x1010 : 0x3232), fb = __byte_perm(sb, 0, w < 2 ? 0x1010 : 0x3232);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t fr[4] = {mul_half2(ha[2 * k], fa), mul_half2(hb[2 * k], fb), mul_half2(ha[2 * k + 1], fa), mul_half2(hb[2 * k + 1], fb)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], fr, qf[nt][4 * w + 2 * k], qf[nt][4 * w + 2 * k + 1]);
+              }
+            }
+          }
+          // ---- softmax: s[nt] = (key kq: rows 2 t, 2 t + 1), (key 8 + kq: the same rows)
+          bool seen[NT][4];
+          bool over = false;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              s[nt][e] *= mul[nt][e & 1];
+              seen[nt][e] = true;
+              if (tail) seen[nt][e] = slot_seen(vis[nt][e & 1], pos0 + kq + 8 * (e >> 1) - sg.ctx);
+              over |= seen[nt][e] && s[nt][e] > m[nt][e & 1] + kLag;
+            }
+          if (__any_sync(0xffffffffu, over)) {           // some row's reference maximum has to move
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float mx = fmaxf(seen[nt][h] ? s[nt][h] : -INFINITY, seen[nt][2 + h] ? s[nt][2 + h] : -INFINITY);
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                if (mx > m[nt][h] + kLag) {
+                  const float corr = ex2(m[nt][h] - mx); // 0 the first time, when there is nothing to scale
+                  m[nt][h] = mx;
+                  l[nt][h] *= corr;
+#pragma unroll
+                  for (int jj = 0; jj < 8; ++jj) { o[nt][jj][h] *= corr; o[nt][jj][2 + h] *= corr; }
+                }
+              }
+          }
+          uint32_t p0[NT], p1[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float mu = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1] - kLift;
+              p[e] = seen[nt][e] ? ex2(s[nt][e] - mu) : 0.f;
+            }
+            l[nt][0] += p[0] + p[2];
+            l[nt][1] += p[1] + p[3];
+            p0[nt] = transpose8(pack_half2(p[0], p[1]));
+            p1[nt] = transpose8(pack_half2(p[2], p[3]));
+          }
+          // ---- O^T: block g of keys t, t + 4 and t + 8, t + 12
+          uint32_t sc[2];
+          uint2 vc[4];
+          {
+            uint32_t b4[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              vc[k] = *reinterpret_cast<const uint2*>(tile + v_codes + k * 4 * 64);
+              b4[k] = tile[v_scales + k * 4 * 8];
+            }
+            if (tail) {
+              // Values nobody reads are left out of the product by a scale of zero (0 x NaN), and so is a NaN that some nodes read: it
+              // turns block g of those nodes' outputs into NaN by hand.
+              uint32_t nan = 0;                          // bit per key of the group
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int slot = pos0 + t + 4 * k - sg.ctx;
+                if (slot < 0) continue;
+                const bool live = slot < a.Ns && ((__ldg(usedw + (slot >> 5)) >> (slot & 31)) & 1u);
+                if (live && (b4[k] & 0x7Fu) == 0x7Fu) nan |= 1u << (t + 4 * k);
+                if (!live || (b4[k] & 0x7Fu) == 0x7Fu) b4[k] = 0;
+              }
+              if (__any_sync(0xffffffffu, nan != 0)) {
+                nan |= __shfl_xor_sync(0xffffffffu, nan, 1);
+                nan |= __shfl_xor_sync(0xffffffffu, nan, 2);     // block g, all sixteen keys
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) {
+                    bool hit = false;
+                    for (int k = 0; k < 16; ++k) hit |= ((nan >> k) & 1u) && slot_seen(vis[nt][h], pos0 + k - sg.ctx);
+                    if (hit)
+#pragma unroll
+                      for (int jj = 0; jj < 8; ++jj) o[nt][jj][h] = o[nt][jj][2 + h] = __int_as_float(0x7FC00000);
+                  }
+              }
+            }
+            sc[0] = e4m3x2_to_half2(b4[0] | b4[1] << 8);
+            sc[1] = e4m3x2_to_half2(b4[2] | b4[3] << 8);
+          }
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {                  // codes 8 w .. 8 w + 7 of the block
+            uint32_t ev[2][4], od[2][4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t x = w ? vc[2 * k].y : vc[2 * k].x, y = w ? vc[2 * k + 1].y : vc[2 * k + 1].x;
+              e2m1x8_to_half2((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), ev[k]);
+              e2m1x8_to_half2(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), od[k]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t fr[4] = {mul_half2(ev[0][i], sc[0]), mul_half2(od[0][i], sc[0]), mul_half2(ev[1][i], sc[1]), mul_half2(od[1][i], sc[1])};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], fr, p0[nt], p1[nt]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.empty[st]);
+      }
+      // ---- the warps' parts meet: maxima and sums, then the outputs of eight rows at a time
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x = l[nt][h];
+          x += __shfl_xor_sync(0xffffffffu, x, 4);
+          x += __shfl_xor_sync(0xffffffffu, x, 8);
+          x += __shfl_xor_sync(0xffffffffu, x, 16);
+          if (g == 0) { sm.stat[warp][nt * 8 + 2 * t + h][0] = m[nt][h]; sm.stat[warp][nt * 8 + 2 * t + h][1] = x; }
+        }
+      asm volatile("bar.sync 1, %0;\n" ::"r"(C::kWarps * 32) : "memory");
+      const bool whole = sg.nslots == 1;                 // the only segment of its unit: these are the final outputs
+      const bool bad = sg.n > 0 && *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[nseg & 15u]) != 0;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int lr = 2 * t + h;
+          float mx = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < C::kWarps; ++w) mx = fmaxf(mx, sm.stat[w][nt * 8 + lr][0]);
+          const float f = m[nt][h] == -INFINITY ? (l[nt][h] == 0.f ? 0.f : 1.f) : ex2(m[nt][h] - mx);
+#pragma unroll
+          for (int jj = 0; jj < 8; ++jj)
+            *reinterpret_cast<float2*>(red + (warp * 8 + lr) * C::kRedRow + jj * 16 + g * 2) = make_float2(o[nt][jj][h] * f, o[nt][jj][2 + h] * f);
+        }
+        asm volatile("bar.sync 1, %0;\n" ::"r"(C::kWarps * 32) : "memory");
+        for (int e = tid; e < 8 * 64; e += C::kWarps * 32) {     // row e / 64, elements 2 (e % 64) and the next
+          const int lr = e >> 6, pr = e & 63, r = sg.rt * a.R + nt * 8 + lr;
+          if (r >= GN) continue;
+          float mx = -INFINITY, lt = 0.f;
+#pragma unroll
+          for (int w = 0; w < C::kWarps; ++w) mx = fmaxf(mx, sm.stat[w][nt * 8 + lr][0]);
+          float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < C::kWarps; ++w) {
+            const float mw = sm.stat[w][nt * 8 + lr][0], lw = sm.stat[w][nt * 8 + lr][1];
+            lt += lw * (mw == -INFINITY ? 1.f : ex2(mw - mx));
+            const float2 v = *reinterpret_cast<const float2*>(red + (w * 8 + lr) * C::kRedRow + (pr & 7) * 16 + (pr >> 3) * 2);
+            sum.x += v.x;
+            sum.y += v.y;
+          }
+          const float inv = bad ? 0.f : row_inverse(lt) * a.v_mul;
+          const float2 val = bad ? make_float2(0.f, 0.f) : make_float2(sum.x * inv, sum.y * inv);
+          const float l2 = row_lse2(mx == -INFINITY ? 0.f : mx, lt);
+          if (whole) {
+            const int hl = r / a.N, node = r - hl * a.N;
+            const size_t row = ((size_t)sg.b * a.N + node) * a.Hq + (size_t)sg.hkv * a.G + hl;
+            if (a.out_bf16) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(val.x, val.y);
+              reinterpret_cast<__nv_bfloat162*>(a.out)[row * 64 + pr] = v;
+            } else {
+              reinterpret_cast<float2*>(a.out)[row * 64 + pr] = val;
+            }
+            if (pr == 0 && a.lse) a.lse[row] = bad ? 0.f : l2 * kLn2;
+          } else {
+            const int rl = nt * 8 + lr;
+            float* slot = a.part_o + (size_t)sg.slot * a.R * kDh;
+            *reinterpret_cast<float2*>(slot + ((size_t)(pr >> 1) * a.R + rl) * 4 + (pr & 1) * 2) = val;
+            if (pr == 0) a.part_lse[(size_t)sg.slot * a.R + rl] = bad ? INFINITY : l2;
+          }
+        }
+        asm volatile("bar.sync 1, %0;\n" ::"r"(C::kWarps * 32) : "memory");
+      }
+      if (whole && tid == 0) a.part_lse[(size_t)sg.slot * a.R] = bad ? INFINITY : 0.f;
+      if (sg.n > 0) ++nseg;
+    }
+    if (!ok) sm.timed_out = 1;
+  }
+  __syncthreads();
+  if (tid == 0) a.cta_code[blockIdx.x] = (int)sm.timed_out;      // the merge kernel turns this into status words
+}
+
+// ---- combination ---------------------------------------------------------------------------
+// A thread takes one row of a unit and four columns; a slot holds its rows by groups of four columns, [column group][row][4], so a warp reads
+// 512 contiguous bytes.  Slots are taken in order (the result for a given decomposition is reproducible), weights 2^(lse - max lse).  A slot whose
+// log-sum-exp is +inf (no sum gives that) met a page that does not exist.
+__global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnArgs a) {
+  constexpr int kBatch = 8;
+  pdl_wait();          // launched as a programmatic dependent of the attention kernel: its slots are complete from here on
+  pdl_trigger();
+  const int upb = a.Hkv * a.RT, per_unit = a.R * 32;
+  const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long uu = e / per_unit;
+  if (uu >= (long long)a.B * upb) return;
+  const int u = (int)uu, i = (int)(e - uu * per_unit);
+  const int cg = i / a.R, r = i - cg * a.R;
+  const int b = u / upb, rem = u - b * upb;
+  const int hkv = rem / a.RT, rt = rem - hkv * a.RT, rg = rt * a.R + r;
+  const int cx = a.ctx_len[b], cr = a.cache_row[b];
+  const int2 sl = a.unit_slots[u];       // meaningless for a sequence that fails its check
+  const int st = seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos);
+  const float* lp = a.part_lse + (size_t)sl.x * a.R + (sl.y == 1 || rg >= a.G * a.N ? 0 : r);
+  float mx = -INFINITY;
+  if (st == LUMO_SEQ_OK)
+    for (int s = 0; s < sl.y; ++s) mx = fmaxf(mx, lp[(size_t)s * a.R]);
+  const bool bad = mx == INFINITY;
+  if (i < 32 && rem == 0 && a.status) {  // one warp a sequence
+    int late = 0;
+    for (int c = i; c < a.C; c += 32) late |= a.cta_code[c];
+    late = __any_sync(0xffffffffu, late);
+    if (i == 0) a.status[b] = st != LUMO_SEQ_OK ? st : (late ? (int)LUMO_SEQ_TIMEOUT : (bad ? (int)LUMO_SEQ_BAD_PAGE : (int)LUMO_SEQ_OK));
+  }
+  if (rg >= a.G * a.N) return;
+  const int hl = rg / a.N, node = rg - hl * a.N;
+  const size_t row = ((size_t)b * a.N + node) * a.Hq + (size_t)hkv * a.G + hl;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float lse = 0.f;
+  if (st == LUMO_SEQ_OK && sl.y == 1) return;      // a single segment: the attention kernel has written the outputs
+  if (st == LUMO_SEQ_OK && !bad) {
+    const float4* op = reinterpret_cast<const float4*>(a.part_o) + ((size_t)sl.x * 32 + cg) * a.R + r;
+    float den = 0.f;
+    for (int s0 = 0; s0 < sl.y; s0 += kBatch) {
+      float4 v[kBatch];
+      float w[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const bool in = s0 + k < sl.y;
+        w[k] = in ? lp[(size_t)(s0 + k) * a.R] : -INFINITY;
+        v[k] = in ? op[(size_t)(s0 + k) * 32 * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (w[k] == -INFINITY) continue; // none, or a slot without keys for this row
+        const float x = mx == -INFINITY ? w[k] : ex2(w[k] - mx);       // (no maximum: every weight is a NaN)
+        den += x;
+        acc.x = fmaf(x, v[k].x, acc.x); acc.y = fmaf(x, v[k].y, acc.y);
+        acc.z = fmaf(x, v[k].z, acc.z); acc.w = fmaf(x, v[k].w, acc.w);
+      }
+    }
+    const float inv = row_inverse(den);
+    acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    lse = den == 0.f ? -INFINITY : (mx + log2f(den)) * kLn2;
+  }
+  if (a.out_bf16) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(acc.x, acc.y), y = __floats2bfloat162_rn(acc.z, acc.w);
+    reinterpret_cast<uint2*>(a.out)[row * 32 + cg] = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  } else {
+    reinterpret_cast<float4*>(a.out)[row * 32 + cg] = acc;
+  }
+  if (a.lse && cg == 0) a.lse[row] = lse;
+}
+
+template <int NT>
+cudaError_t launch_small(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+  static bool configured[kMaxDevices] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < kMaxDevices && !configured[dev]) {
+    e = cudaFuncSetAttribute(kv4_attn_small_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Small<NT>::kBytes);
+    if (e != cudaSuccess) return e;
+    configured[dev] = true;
+  }
+  return launch_kernel(kv4_attn_small_kernel<NT>, dim3(plan.a.C), dim3(Small<NT>::kThreads), Small<NT>::kBytes, st, pdl, plan.a);
+}
+
+int rows_per_tile(int G, int N) { return G * N <= 8 ? 8 : 16; }
+
+}  // namespace
+
+static long long kv4_units(int B, int N, int Hq, int Hkv) {
+  const int G = Hq / Hkv, R = rows_per_tile(G, N);
+  return (long long)B * Hkv * ((G * N + R - 1) / R);
+}
+
+// workspace: partial outputs [slots][R][128], log-sum-exps [slots][R], CTA codes, the units' slots
+static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms) {
+  const int R = rows_per_tile(Hq / Hkv, N);
+  const size_t units = (size_t)kv4_units(B, N, Hq, Hkv), ctas = n_splits > 0 ? units * n_splits : (size_t)sms;
+  const size_t slots = n_splits > 0 ? ctas : units + ctas;
+  return round256(slots * R * kDh * 4) + round256(slots * R * 4) + round256(ctas * 4) + round256(units * sizeof(int2));
+}
+
+void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
+              int n_splits, void* work, int sms, Kv4Plan* plan) {
+  Kv4AttnArgs& a = plan->a;
+  a.pages = reinterpret_cast<const unsigned char*>(p.pages); a.q = p.q; a.out = p.out; a.lse = p.lse; a.status = p.status;
+  a.ctx_len = s.ctx_len; a.cache_row = s.cache_row; a.table = s.table; a.vis = vis; a.used = used; a.q_stride = q_stride;
+  a.B = s.B; a.N = s.N; a.Ns = s.Ns; a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.Hq / s.Hkv;
+  a.R = rows_per_tile(a.G, a.N);
+  a.RT = (a.G * a.N + a.R - 1) / a.R;
+  a.n_rows = s.n_rows; a.max_pages = s.max_pages; a.n_pages = s.n_pages; a.page_log2 = s.page_log2; a.max_pos = s.max_pages << s.page_log2;
+  const size_t units = (size_t)s.B * s.Hkv * a.RT, ctas = n_splits > 0 ? units * n_splits : (size_t)sms;
+  const size_t slots = n_splits > 0 ? ctas : units + ctas;
+  a.S = n_splits; a.C = (int)ctas; a.out_bf16 = out_bf16;
+  a.scale_log2 = ldexpf(scale * kLog2e, s.k_exp);
+  a.v_mul = ldexpf(1.f, s.v_exp);
+  unsigned char* w = reinterpret_cast<unsigned char*>(work);
+  a.part_o = reinterpret_cast<float*>(w); w += round256(slots * a.R * kDh * 4);
+  a.part_lse = reinterpret_cast<float*>(w); w += round256(slots * a.R * 4);
+  a.cta_code = reinterpret_cast<int32_t*>(w); w += round256(ctas * 4);
+  a.unit_slots = reinterpret_cast<int2*>(w);
+  plan->kind = 0;
+}
+
+cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+  return plan.a.R == 8 ? launch_small<1>(plan, pdl, st) : launch_small<2>(plan, pdl, st);
+}
+
+cudaError_t launch_kv4_merge(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+  const long long threads = (long long)plan.a.B * plan.a.Hkv * plan.a.RT * plan.a.R * 32;
+  return launch_kernel(kv4_merge_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, pdl, plan.a);
+}
+
+}  // namespace lumo
