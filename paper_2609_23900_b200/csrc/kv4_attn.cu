@@ -16,221 +16,11 @@
 #include <cuda_runtime.h>
 
 #include "internal.h"
-#include "kv4.h"
+#include "kv4_attn.h"
 
 namespace lumo {
 
 namespace {
-
-constexpr int kDh = 128;
-constexpr int kKeys = 128;            // keys per tile
-constexpr int kTileBytes = kKeys * 2 * kKv4Entry;   // 18432: keys and values, codes and scales
-constexpr int kSeqCache = 64;         // sequences whose context length, cache row and tile count are kept in shared memory
-constexpr float kLag = 8.f;           // the reference maximum moves when exceeded by more than this (log2 units)
-constexpr float kLift = 6.f;          // probabilities are held as 2^kLift times themselves: at most 2^14 in f16, and what f16 drops is below 2^-30
-constexpr uint32_t kSpinLimit = 1u << 24;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory");
-}
-// Bounded wait: false if the phase did not complete within the spin limit.
-__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity) {
-  const uint32_t addr = smem_u32(bar);
-  for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
-    uint32_t done;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(done) : "r"(addr), "r"(parity) : "memory");
-    if (done) return true;
-  }
-  return false;
-}
-// untiled bulk copy into shared memory: both addresses 16-byte aligned, a multiple of 16 bytes; completion counted on `bar`
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, unsigned long long* bar, uint64_t policy) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;\n"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy) : "memory");
-}
-__device__ __forceinline__ uint64_t l2_evict_first_policy() {
-  uint64_t p;
-  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(p));
-  return p;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
-  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-// (base-2 log-sum-exp of a row from its reference maximum and lifted sum; a NaN stays one, a row without keys gives -inf)
-__device__ __forceinline__ float row_lse2(float m, float l) { return l == 0.f ? -INFINITY : m - kLift + log2f(l); }
-__device__ __forceinline__ float row_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
-
-// The power of two that takes a query row to f16: its largest magnitude becomes 2^14 to 2^15.  `top`: that magnitude's bits.
-__device__ __forceinline__ int query_exponent(uint32_t top) {
-  const int e = (int)(top >> 23) - 127;
-  return min(14 - e, 120);
-}
-
-// ---- work decomposition ----------------------------------------------------------------
-// Units are numbered u = (b * Hkv + hkv) * RT + rt; unit u owns nt(b) tiles (0 for a sequence that fails its check).  Automatic mode: the
-// units are laid end to end on a line, each preceded by `cost` idle positions (the price of starting it, in tiles); CTA c owns the
-// positions [c * per, (c + 1) * per), works on the tiles among them, and the slot of a segment is u + c (strictly increasing along the line,
-// so unique).  Fixed mode (S partitions): CTA c owns partition c mod S of unit c / S, slot c.
-struct SeqCache { int ctx[kSeqCache], row[kSeqCache], nt[kSeqCache]; };
-struct Segment {
-  int b, hkv, rt;     // unit
-  int t0, n;          // first tile within the unit, tile count (n = 0 possible in fixed mode)
-  int slot;
-  int unit, slot0, nslots;   // the unit, and the slots all its segments write (ascending along the key range)
-  int ctx, crow;
-};
-
-__device__ __forceinline__ int seq_tiles(const Kv4AttnArgs& a, int cx, int cr) {
-  return seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos) == LUMO_SEQ_OK ? (cx + a.Ns + kKeys - 1) / kKeys : 0;
-}
-__device__ __forceinline__ void fill_seq_cache(const Kv4AttnArgs& a, SeqCache& s) {
-  if (threadIdx.x < kSeqCache && threadIdx.x < a.B) {
-    const int cx = a.ctx_len[threadIdx.x], cr = a.cache_row[threadIdx.x];
-    s.ctx[threadIdx.x] = cx; s.row[threadIdx.x] = cr; s.nt[threadIdx.x] = seq_tiles(a, cx, cr);
-  }
-}
-
-template <int kCost, int kMinTiles, int kSlack>
-struct Work {
-  const Kv4AttnArgs& a;
-  const SeqCache& sc;
-  int b = 0, q = 0;   // current sequence, unit within the sequence
-  int g = 0, g_end = 0;       // next position on the line, end of this CTA's share (the host bounds the line below 2^31)
-  int g_unit = 0;     // position at which the current unit's stretch (idle prefix, then its tiles) starts
-  int nt = 0;         // tiles per unit of the current sequence
-  int per = 1;        // automatic mode: positions per CTA
-  int parts;          // partitions per unit when CTA c owns partition c mod parts of unit c / parts; 0: shares of the line
-  bool fixed_done = false;
-
-  __device__ __forceinline__ int tiles_of(int bb, int* ctx, int* crow) const {
-    if (bb < kSeqCache) { *ctx = sc.ctx[bb]; *crow = sc.row[bb]; return sc.nt[bb]; }
-    *ctx = a.ctx_len[bb];
-    *crow = a.cache_row[bb];
-    return seq_tiles(a, *ctx, *crow);
-  }
-
-  __device__ Work(const Kv4AttnArgs& args, const SeqCache& cache) : a(args), sc(cache), parts(args.S) {
-    if (parts > 0) return;
-    const int upb = a.Hkv * a.RT;       // units per sequence
-    int total = 0, most = 0, cx, cr;
-    for (int bb = 0; bb < a.B; ++bb) {
-      const int n = tiles_of(bb, &cx, &cr);
-      if (n > 0) total += (n + kCost) * upb;
-      most = max(most, n);
-    }
-    per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
-    // Short contexts: when there is a CTA for every unit and no unit is much longer than an even share, units stay whole: nothing
-    // is cut, and with one segment per unit the outputs are final when they leave this kernel.
-    if (a.B * upb <= (int)gridDim.x && most <= per + kSlack) { parts = 1; return; }
-    if (per < kMinTiles) per = kMinTiles;
-    g = (int)blockIdx.x * per;
-    g_end = g + per < total ? g + per : total;
-    int acc = 0;                        // the unit whose stretch holds position g
-    for (b = 0; b < a.B; ++b) {
-      nt = tiles_of(b, &cx, &cr);
-      const int span = nt > 0 ? (nt + kCost) * upb : 0;
-      if (g < acc + span) { q = (g - acc) / (nt + kCost); g_unit = acc + q * (nt + kCost); break; }
-      acc += span;
-    }
-  }
-
-  // next segment of this CTA; false when the share is exhausted
-  __device__ __forceinline__ bool next(Segment* s) {
-    const int upb = a.Hkv * a.RT;
-    if (parts > 0) {
-      if (fixed_done) return false;
-      fixed_done = true;
-      const int u = blockIdx.x / parts, part = blockIdx.x - u * parts;
-      s->b = u / upb;
-      if (s->b >= a.B) return false;
-      const int r = u - s->b * upb;
-      s->hkv = r / a.RT; s->rt = r - s->hkv * a.RT;
-      const int n_all = tiles_of(s->b, &s->ctx, &s->crow);
-      s->t0 = (int)(((long long)part * n_all) / parts);
-      s->n = (int)(((long long)(part + 1) * n_all) / parts) - s->t0;
-      s->slot = blockIdx.x;
-      s->unit = u; s->slot0 = u * parts; s->nslots = parts;
-      return n_all > 0;
-    }
-    while (g < g_end && b < a.B) {
-      if (nt == 0 || g >= g_unit + nt + kCost) {         // move to the next unit (skipping sequences without tiles)
-        if (nt > 0) g_unit += nt + kCost;
-        if (nt == 0 || ++q == upb) {
-          q = 0;
-          int cx, cr;
-          do { ++b; nt = b < a.B ? tiles_of(b, &cx, &cr) : 0; } while (b < a.B && nt == 0);
-        }
-        continue;
-      }
-      const int first = g_unit + kCost;                  // position of the unit's tile 0
-      const int lo = g > first ? g : first;
-      const int hi = first + nt < g_end ? first + nt : g_end;
-      g = g_unit + nt + kCost < g_end ? g_unit + nt + kCost : g_end;
-      if (lo >= hi) continue;                            // only idle positions of this unit fall into the share
-      const int u = b * upb + q;
-      s->b = b; s->hkv = q / a.RT; s->rt = q - s->hkv * a.RT;
-      tiles_of(b, &s->ctx, &s->crow);
-      s->t0 = lo - first;
-      s->n = hi - lo;
-      s->slot = u + blockIdx.x;
-      s->unit = u;
-      s->slot0 = u + first / per;
-      s->nslots = (first + nt - 1) / per - first / per + 1;
-      return true;
-    }
-    return false;
-  }
-};
-
-// Stages one tile: a bulk copy per page that holds positions below ctx + Ns (the lanes of the loading warp take a page each).  A page
-// number out of range sets *bad_page, and nothing is copied for it.
-__device__ __forceinline__ void load_tile(const Kv4AttnArgs& a, const Segment& sg, int tile, uint32_t dst, unsigned long long* full, uint32_t* bad_page,
-                                          uint64_t policy) {
-  const int lane = threadIdx.x & 31;
-  const int page = 1 << a.page_log2, per_tile = kKeys >> a.page_log2;
-  const int pos = tile * kKeys + (lane << a.page_log2);
-  const bool mine = lane < per_tile && pos < sg.ctx + a.Ns;
-  int pg = -1;
-  if (mine) pg = __ldg(a.table + (size_t)sg.crow * a.max_pages + (pos >> a.page_log2));
-  const bool ok = mine && pg >= 0 && pg < a.n_pages;
-  const uint32_t bytes = page * 2 * kKv4Entry;
-  const unsigned good = __ballot_sync(0xffffffffu, ok);
-  const bool bad = __any_sync(0xffffffffu, mine && !ok);
-  if (lane == 0) {
-    if (bad) *reinterpret_cast<volatile uint32_t*>(bad_page) = 1;
-    mbar_expect_tx(full, __popc(good) * bytes);
-  }
-  __syncwarp();
-  if (ok) bulk_load(dst + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, 0), bytes, full, policy);
-}
-
-__device__ __forceinline__ bool slot_seen(const uint32_t* row, int s) {        // s: suffix slot; below 0: context
-  return s < 0 || (s < kMaxAttnSlots && ((__ldg(row + (s >> 5)) >> (s & 31)) & 1u));
-}
 
 // ---- register form -----------------------------------------------------------------------
 // For up to 8 NT query rows per unit (a token or a short tree of one request times its head group).  Bound by the cache's bytes, so the point is
@@ -378,6 +168,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
         if (C::kWarps == 16 && (int)(it & 1u) != warp >> 3) continue;           // the other eight warps' tile
         const uint32_t st = it % C::kStages;
         if (ok) ok = mbar_wait(&sm.full[st], (it / C::kStages) & 1u);
+        ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
         const int pos0 = (sg.t0 + j) * kKeys + c0;       // the group's first position
         if (ok && pos0 < sg.ctx + a.Ns) {
           const unsigned char* tile = smem + st * kTileBytes;
@@ -667,7 +458,8 @@ cudaError_t launch_small(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   return launch_kernel(kv4_attn_small_kernel<NT>, dim3(plan.a.C), dim3(Small<NT>::kThreads), Small<NT>::kBytes, st, pdl, plan.a);
 }
 
-int rows_per_tile(int G, int N) { return G * N <= 8 ? 8 : 16; }
+// rows of a row tile: the register form up to sixteen, the tensor-memory form (kv4_attn_tc.cu) beyond
+int rows_per_tile(int G, int N) { return G * N <= 8 ? 8 : G * N <= 16 ? 16 : 128; }
 
 }  // namespace
 
@@ -704,10 +496,10 @@ void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, cons
   a.part_lse = reinterpret_cast<float*>(w); w += round256(slots * a.R * 4);
   a.cta_code = reinterpret_cast<int32_t*>(w); w += round256(ctas * 4);
   a.unit_slots = reinterpret_cast<int2*>(w);
-  plan->kind = 0;
 }
 
 cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+  if (plan.a.R == 128) return launch_kv4_attn_tc(plan, pdl, st);
   return plan.a.R == 8 ? launch_small<1>(plan, pdl, st) : launch_small<2>(plan, pdl, st);
 }
 
