@@ -2,20 +2,24 @@
 // and how the work is dealt out.  A persistent CTA per SM; the query rows of all heads that share the KV head sit in one 128-row tile
 // (row = head-in-group * N + node).
 //
-//   warps 0-7    softmax: a query row (= tensor-memory lane) is shared by two threads (warps w and w + 4), 64 keys each.  A thread reads its
-//                logits, applies visibility by selection, exponentiates against a REFERENCE maximum, which moves (with a rescale of the
-//                accumulator) only when exceeded by more than 2^kLag, and stores the probabilities as f16 in the first half of the
-//                columns its own logits stood in: that is the A operand of the second product, where it lies
-//   warps 8-11   codes to operands: 32 codes and two scales at a time from the staged page blocks to f16 in shared memory, K and V tiles
-//                alike ([128 keys x 128 bytes] per half of the head, 128-byte swizzle; two buffers each).  Eight lanes read 128
-//                contiguous bytes of codes and write eight different 16-byte columns
-//   warp 12      loader: bulk copies of a head's page blocks into a ring of five tiles
-//   warp 13      issuer: S = Q K^T into one of two S buffers (one tile ahead of the probabilities), O += P V into an accumulator that
-//                stays in tensor memory for the whole segment.  Q and P are A operands in tensor memory
+//   warps 0-7    softmax: two groups of four warps take the tiles in turn, a thread a query row (= tensor-memory lane) of 128 keys, so that on
+//                every scheduler one warp looks for its tile's maxima while the other keeps the exponentials' unit busy.  A thread applies
+//                visibility by selection, exponentiates against the row's REFERENCE maximum (shared by the groups; it moves, with a
+//                rescale of the accumulator, only when exceeded by more than 2^kLag) and stores the probabilities as f16 over logits that
+//                it has read: the A operand of the second product, where it lies
+//   warps 8-15   codes to operands, four warps for the keys and four for the values: 32 codes and two scales at a time from the staged
+//                page blocks to f16 in shared memory ([128 keys x 128 bytes] per half of the head, 128-byte swizzle; two buffers each)
+//   warps 16, 17 loaders: bulk copies of a head's page blocks into two rings of three tiles, one of keys and one of values (the values
+//                are used two tiles later)
+//   warps 18, 19 issuers: S = Q K^T into one of three S buffers (up to two tiles ahead of the probabilities, so that a group finds its next
+//                logits ready), and O += P V into an accumulator that stays in tensor memory for the whole segment.  The tensor core takes
+//                few instructions ahead, and a wait costs its issuer 150 cycles or more even when nothing is awaited (measured): so there
+//                are two, each with one wait and one commit a tile, and one issues while the other waits.  Q lies in shared memory: the
+//                tensor core reads it from there at the same rate (1024 cycles for both products either way, measured)
 //
 // What bounds it: shared memory carries 164 KB a tile (codes written and read, operands written and read by the tensor core), 1312 cycles at
 // 128 bytes a cycle; the two products take 1024 cycles, the exponentials 1024 on their own units, and the instructions of the softmax and
-// of the conversion about 1100 of the four schedulers.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the
+// of the conversion about 1000 of the four schedulers.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the
 // memory.
 #include "kv4_attn.h"
 
@@ -24,29 +28,33 @@ namespace lumo {
 namespace {
 
 constexpr int kRows = 128;            // query rows per unit = tensor-memory lanes
-constexpr int kSoftmaxWarps = 8, kConvertWarps = 4;
-constexpr int kLoadWarp = kSoftmaxWarps + kConvertWarps, kIssueWarp = kLoadWarp + 1;
-constexpr int kThreads = 32 * (kIssueWarp + 1);
-constexpr int kStages = 5;            // ring of staged tiles
-constexpr int kTmemCols = 512;        // S buffers (and P in them): 0..127, 128..255; O: 256..383; Q (f16 pairs): 384..447
-constexpr int kColO = 256;
-constexpr int kColQ = 384;
+constexpr int kSoftmaxWarps = 8, kGroupWarps = 4;     // four warps: one softmax group, the keys' or the values' conversion
+constexpr int kLoadWarp = kSoftmaxWarps + 2 * kGroupWarps, kIssueWarp = kLoadWarp + 2;   // two of each
+constexpr int kThreads = 32 * (kIssueWarp + 2);
+constexpr int kStages = 3;            // staged tiles per ring
+constexpr int kRawBytes = kKeys * kKv4Entry;            // 9216
+constexpr int kBufs = 3;              // S buffers
+constexpr int kTmemCols = 512;        // S buffers (and P in them): 0..383; O: 384..511
+constexpr int kColO = kBufs * kKeys;
 constexpr int kHalfBytes = 16384;     // one dh half of an operand tile: [128 keys x 128 B]
 constexpr int kOpBytes = 2 * kHalfBytes;
-constexpr int kOffK = 0;              // two K tiles, two V tiles, the ring
+constexpr int kOffK = 0;              // two K tiles, two V tiles, Q, the ring
 constexpr int kOffV = 2 * kOpBytes;
-constexpr int kOffRaw = 4 * kOpBytes;
-constexpr int kOffCtl = kOffRaw + kStages * kTileBytes;
+constexpr int kOffQ = 4 * kOpBytes;
+constexpr int kOffRaw = 5 * kOpBytes;
+constexpr int kOffCtl = kOffRaw + 2 * kStages * kRawBytes;
 struct Ctl {
-  unsigned long long raw_full[kStages], raw_empty[kStages];
-  unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2];
-  unsigned long long s_full[2], p_full[2];
-  unsigned long long q_full, o_free, drain;
+  unsigned long long raw_full[2][kStages], raw_empty[2][kStages];   // [keys, values]
+  unsigned long long k_full[2], v_full[2], v_empty[2];
+  unsigned long long s_full[kBufs];   // logits complete (and the K tile read)
+  unsigned long long pv_full[kBufs];  // probabilities and values complete
+  unsigned long long q_full, o_free, drain[2];
   uint32_t tmem_base;
   uint32_t timed_out;
   uint32_t bad_page[16];              // by segment number mod 16: the loader is never that far ahead
   SeqCache seq;
-  float xchg[2][kRows];               // [key half][row]: what the two threads of a row tell one another
+  float ref[kRows];                   // the rows' reference maxima
+  float xchg[2][kRows];               // [group][row]: what the two threads of a row tell one another
   uint32_t nan_blocks[2][kRows / 4];  // [V buffer][key], a byte each: blocks of values that are NaN in a suffix position
 };
 constexpr int kSmemBytes = kOffCtl + (int)sizeof(Ctl);
@@ -77,6 +85,13 @@ __device__ __forceinline__ void umma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// product with both operands in shared memory
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+      ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
 __device__ __forceinline__ void umma_commit(unsigned long long* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -90,29 +105,52 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
-// whether any of the 64 threads of a pair of warps says yes (all of them get the answer)
-__device__ __forceinline__ bool pair_any(int bar, bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\n"
-      "barrier.cta.red.or.pred q, %1, 64, p;\n"
-      "selp.u32 %0, 1, 0, q;\n}\n"
-      : "=r"(r) : "r"(bar), "r"((uint32_t)x) : "memory");
-  return r != 0;
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void pair_sync(int bar) { asm volatile("barrier.cta.sync %0, 64;\n" ::"r"(bar) : "memory"); }
+
+__device__ __forceinline__ void pair_arrive(int bar) { asm volatile("barrier.cta.arrive %0, 64;\n" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;\n"
+      : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
 
 // Visibility of 64 consecutive keys from suffix slot s0 on (negative: keys of the committed context, always visible), from a
 // node's 256-bit row over the suffix.
@@ -141,15 +179,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.raw_full[s], 1); mbar_init(&sm.raw_empty[s], kConvertWarps); }
+    for (int s = 0; s < 2 * kStages; ++s) { mbar_init(&sm.raw_full[0][s], 1); mbar_init(&sm.raw_empty[0][s], kGroupWarps); }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&sm.k_full[s], kConvertWarps); mbar_init(&sm.v_full[s], kConvertWarps);
-      mbar_init(&sm.k_empty[s], 1); mbar_init(&sm.v_empty[s], 1);
-      mbar_init(&sm.s_full[s], 1); mbar_init(&sm.p_full[s], kSoftmaxWarps);
+      mbar_init(&sm.k_full[s], kGroupWarps); mbar_init(&sm.v_full[s], kGroupWarps);
+      mbar_init(&sm.v_empty[s], 1);
     }
+    for (int s = 0; s < kBufs; ++s) { mbar_init(&sm.s_full[s], 1); mbar_init(&sm.pv_full[s], 2 * kGroupWarps); }
     mbar_init(&sm.q_full, kSoftmaxWarps);
     mbar_init(&sm.o_free, kSoftmaxWarps);
-    mbar_init(&sm.drain, 1);
+    mbar_init(&sm.drain[0], 1);
+    mbar_init(&sm.drain[1], 1);
     sm.timed_out = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -168,162 +207,200 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
   uint32_t it = 0;        // tiles this CTA has started, over all segments: ring stage, buffers and phases
   uint32_t nseg = 0;      // segments with tiles so far: phases of q_full and o_free
 
-  if (warp == kLoadWarp) {
-    // ---------------- loader ----------------
+  if (warp == kLoadWarp || warp == kLoadWarp + 1) {
+    // ---------------- loaders: keys (which = 0) and values (1), a lane a page ----------------
     const uint64_t policy = l2_evict_first_policy();
+    const int page = 1 << a.page_log2, which = warp - kLoadWarp;
+    const uint32_t bytes = page * kKv4Entry;
     while (work.next(&sg)) {
+      const int32_t* entries = a.table + (size_t)sg.crow * a.max_pages + lane;
+      const int first_page = (sg.t0 * kKeys) >> a.page_log2, per_tile = kKeys >> a.page_log2, n_pg = (sg.ctx + a.Ns + page - 1) >> a.page_log2;
+      auto wants = [&](int j) { return lane < per_tile && j < sg.n && first_page + j * per_tile + lane < n_pg; };
+      int next = wants(0) ? __ldg(entries + first_page) : -1;          // page numbers are asked for a tile ahead
       for (int j = 0; j < sg.n; ++j, ++it) {
         const uint32_t st = it % kStages, use = it / kStages;
-        if (use > 0 && ok) ok = mbar_wait(&sm.raw_empty[st], (use - 1) & 1u);
+        const bool wanted = wants(j);
+        const int pg = next;
+        next = wants(j + 1) ? __ldg(entries + first_page + (j + 1) * per_tile) : -1;
+        if (use > 0 && ok) ok = mbar_wait(&sm.raw_empty[which][st], (use - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        if (j == 0 && lane == 0) sm.bad_page[nseg & 15u] = 0;
-        load_tile(a, sg, sg.t0 + j, sbase + kOffRaw + st * kTileBytes, &sm.raw_full[st], &sm.bad_page[nseg & 15u], policy);
+        const bool good = wanted && pg >= 0 && pg < a.n_pages;
+        const unsigned loads = __ballot_sync(0xffffffffu, good);
+        const bool bad = __any_sync(0xffffffffu, wanted && !good);
+        if (lane == 0) {
+          if (j == 0 && !which) sm.bad_page[nseg & 15u] = 0;
+          if (bad && !which) *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[nseg & 15u]) = 1;
+          mbar_expect_tx(&sm.raw_full[which][st], __popc(loads) * bytes);
+        }
+        __syncwarp();
+        if (good)
+          bulk_load(sbase + kOffRaw + (which * kStages + st) * kRawBytes + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, which), bytes,
+                    &sm.raw_full[which][st], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
     }
     // no copy may be on its way when the CTA leaves: the last use of every stage (complete already unless a wait ran out)
-    for (uint32_t s = 0; s < kStages && s < it; ++s) mbar_wait(&sm.raw_full[s], ((it - 1 - s) / kStages) & 1u);
+    for (uint32_t s = 0; s < kStages && s < it; ++s) mbar_wait(&sm.raw_full[which][s], ((it - 1 - s) / kStages) & 1u);
     if (!ok && lane == 0) sm.timed_out = 1u;
   } else if (warp == kIssueWarp) {
-    // ---------------- tensor-core issuer ----------------
-    if (lane == 0) {
-      // S = Q K^T: A = Q in tensor memory, B = K tile (K-major: 128 key rows of 128 B per dh half)
-      auto issue_qk = [&](uint32_t t) {
-        constexpr uint32_t id = umma_idesc(kRows, kKeys, 0);
-        if (ok) ok = mbar_wait(&sm.k_full[t & 1u], (t >> 1) & 1u);
+    // ---------------- issuer of S = Q K^T: both K-major, 128 rows of 128 B per dh half ----------------
+    // (K tile t is announced only when its S buffer is free too, see the conversion; whole warps run these loops, and one lane issues)
+    constexpr uint32_t id = umma_idesc(kRows, kKeys, 0);
+    const uint64_t dq = umma_desc(sbase + kOffQ, 16, 1024), dk = umma_desc(sbase + kOffK, 16, 1024);
+    while (work.next(&sg)) {
+      if (sg.n == 0) continue;
+      if (ok) ok = mbar_wait(&sm.q_full, nseg & 1u);
+      for (int j = 0; j < sg.n; ++j, ++it) {
+        if (ok) ok = mbar_wait(&sm.k_full[it & 1u], (it >> 1) & 1u);
         tc_fence_after();
-        if (!ok) return;
-        const uint32_t kb = sbase + kOffK + (t & 1u) * kOpBytes;
+        const uint64_t kd = dk + (it & 1u) * (kOpBytes >> 4);
+        const uint32_t d = tmem + (it % kBufs) * kKeys;
+        if (ok && elect_one()) {
 #pragma unroll
-        for (int ks = 0; ks < kDh / 16; ++ks)
-          umma_ta(tmem + (t & 1u) * kKeys, tmem + kColQ + ks * 8, umma_desc(kb + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024), id, ks ? 1u : 0u);
-        umma_commit(&sm.s_full[t & 1u]);
-        umma_commit(&sm.k_empty[t & 1u]);
-      };
-      // O += P V: A = P where the logits of its keys stood, B = V tile (MN-major: 128 B of dh per key row, the two dh halves kHalfBytes
-      // apart, 16 keys = 2048 B per K step)
-      auto issue_pv = [&](uint32_t t, bool first) {
-        constexpr uint32_t id = umma_idesc(kRows, kDh, 1);
-        const uint32_t vb = sbase + kOffV + (t & 1u) * kOpBytes, p = tmem + (t & 1u) * kKeys;
-#pragma unroll
-        for (int ks = 0; ks < kKeys / 16; ++ks)
-          umma_ta(tmem + kColO, p + (ks >> 2) * 64 + (ks & 3) * 8, umma_desc(vb + ks * 2048, kHalfBytes, 1024), id, (first && ks == 0) ? 0u : 1u);
-        umma_commit(&sm.v_empty[t & 1u]);
-      };
-      while (work.next(&sg)) {
-        if (sg.n == 0) continue;
-        if (ok) ok = mbar_wait(&sm.q_full, nseg & 1u);
-        issue_qk(it);
-        for (int j = 0; j < sg.n; ++j, ++it) {
-          // the next tile's logits run under this one's softmax; their buffer's last reader was the product before this one
-          if (j + 1 < sg.n) issue_qk(it + 1);
-          if (ok) ok = mbar_wait(&sm.v_full[it & 1u], (it >> 1) & 1u);
-          if (ok) ok = mbar_wait(&sm.p_full[it & 1u], (it >> 1) & 1u);
-          if (j == 0 && nseg > 0 && ok) ok = mbar_wait(&sm.o_free, (nseg - 1) & 1u);
-          tc_fence_after();
-          if (ok) issue_pv(it, j == 0);
+          for (int ks = 0; ks < kDh / 16; ++ks) {
+            constexpr int half16 = kHalfBytes >> 4;
+            umma_ss(d, dq + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, id, ks ? 1u : 0u);
+          }
+          umma_commit(&sm.s_full[it % kBufs]);
         }
-        ++nseg;
+        __syncwarp();
       }
-      if (!ok) {                      // products may still run: they end before tensor memory is freed
-        umma_commit(&sm.drain);
-        mbar_wait(&sm.drain, 0);
-        sm.timed_out = 1u;
-      }
+      ++nseg;
     }
-    __syncwarp();
+    if (!ok) {                        // products may still run: they end before tensor memory is freed
+      if (elect_one()) umma_commit(&sm.drain[0]);
+      mbar_wait(&sm.drain[0], 0);
+      if (lane == 0) sm.timed_out = 1u;
+    }
+  } else if (warp == kIssueWarp + 1) {
+    // ---------------- issuer of O += P V ----------------
+    // A = P in the first half of its S buffer, B = V tile (MN-major: 128 B of dh per key row, the two dh halves kHalfBytes apart, 16 keys =
+    // 2048 B per K step)
+    constexpr uint32_t id = umma_idesc(kRows, kDh, 1);
+    const uint64_t dv = umma_desc(sbase + kOffV, kHalfBytes, 1024);
+    while (work.next(&sg)) {
+      if (sg.n == 0) continue;
+      for (int j = 0; j < sg.n; ++j, ++it) {
+        if (j == 0 && nseg > 0 && ok) ok = mbar_wait(&sm.o_free, (nseg - 1) & 1u);
+        if (ok) ok = mbar_wait(&sm.pv_full[it % kBufs], (it / kBufs) & 1u);
+        tc_fence_after();
+        const uint64_t vd = dv + (it & 1u) * (kOpBytes >> 4);
+        const uint32_t p = tmem + (it % kBufs) * kKeys;
+        if (ok && elect_one()) {
+#pragma unroll
+          for (int ks = 0; ks < kKeys / 16; ++ks) umma_ta(tmem + kColO, p + ks * 8, vd + ks * (2048 >> 4), id, (j == 0 && ks == 0) ? 0u : 1u);
+          umma_commit(&sm.v_empty[it & 1u]);
+        }
+        __syncwarp();
+      }
+      ++nseg;
+    }
+    if (!ok) {
+      if (elect_one()) umma_commit(&sm.drain[1]);
+      mbar_wait(&sm.drain[1], 0);
+      if (lane == 0) sm.timed_out = 1u;
+    }
   } else if (warp >= kSoftmaxWarps) {
-    // ---------------- codes to operands ----------------
-    const int w = warp - kSoftmaxWarps;
+    // ---------------- codes to operands: keys (which = 0) or values (1) ----------------
+    const int which = (warp - kSoftmaxWarps) >> 2, w = warp & 3;
     const int page = 1 << a.page_log2;
-    const int ch = lane & 3;                             // codes [32 ch, 32 ch + 32) of a key: blocks 2 ch and 2 ch + 1
-    const int swap = ch >> 1 ? 2 : 0;                    // the second half of the head in another order: no two lanes meet in a bank
+    // Lane (r, ch): codes [32 ch, 32 ch + 32) of a key, that is blocks 2 ch and 2 ch + 1.  Eight lanes (two keys, all of their codes) read 128
+    // contiguous bytes; the lanes of the head's second half take the key two further, so that the eight write eight different 16-byte columns.
+    const int ch = lane & 3, kr = (lane >> 2) ^ (ch & 2);
+    unsigned long long* full = which ? sm.v_full : sm.k_full;
     while (work.next(&sg)) {
       const uint32_t* usedw = a.used + (size_t)sg.b * 8;
       for (int j = 0; j < sg.n; ++j, ++it) {
         const uint32_t st = it % kStages, buf = it & 1u;
         const int pos0 = (sg.t0 + j) * kKeys;
         const bool tail = pos0 + kKeys > sg.ctx;         // uniform: the tile reaches past the committed context
-        const unsigned char* raw = smem + kOffRaw + st * kTileBytes;
-        if (ok) ok = mbar_wait(&sm.raw_full[st], (it / kStages) & 1u);
-#pragma unroll 1
-        for (int which = 0; which < 2; ++which) {
-          unsigned long long* empty = which ? &sm.v_empty[buf] : &sm.k_empty[buf];
-          if (it >= 2 && ok) ok = mbar_wait(empty, ((it >> 1) - 1) & 1u);
-          ok = __all_sync(0xffffffffu, ok);              // (what follows shuffles: all lanes or none)
-          unsigned char* op = smem + (which ? kOffV : kOffK) + buf * kOpBytes + (ch >> 1) * kHalfBytes;
-          if (ok) {
-            uint4 code[4];
-            uint32_t sc[4];
+        const unsigned char* raw = smem + kOffRaw + (which * kStages + st) * kRawBytes;
+        if (ok) ok = mbar_wait(&sm.raw_full[which][st], (it / kStages) & 1u);
+        ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
+        uint4 code[4];
+        uint32_t sc[4];
+        if (ok) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = w * 32 + i * 8 + (lane >> 2), pi = key >> a.page_log2, r = key & (page - 1);
-              const unsigned char* blk = raw + (pi * 2 + which) * page * kKv4Entry;
-              code[i] = *reinterpret_cast<const uint4*>(blk + r * 64 + ch * 16);
-              sc[i] = *reinterpret_cast<const unsigned short*>(blk + page * 64 + r * 8 + ch * 2);
-            }
-            if (which && tail) {
-              // Values nobody reads get a scale of zero (0 x NaN), and so does a NaN that some nodes read: the softmax warps, which know
-              // who does, hear of it by a bit per block.
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int key = w * 32 + i * 8 + (lane >> 2), slot = pos0 + key - sg.ctx;
-                uint32_t bits = 0;
-                if (slot >= 0) {
-                  const bool live = slot < a.Ns && ((__ldg(usedw + (slot >> 5)) >> (slot & 31)) & 1u);
-                  const bool n0 = (sc[i] & 0x7Fu) == 0x7Fu, n1 = (sc[i] & 0x7F00u) == 0x7F00u;
-                  if (live) bits = ((uint32_t)n0 | (uint32_t)n1 << 1) << (2 * ch);
-                  if (!live) sc[i] = 0;
-                  if (n0) sc[i] &= 0xFF00u;
-                  if (n1) sc[i] &= 0x00FFu;
-                }
-                bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
-                bits |= __shfl_xor_sync(0xffffffffu, bits, 2);
-                if (ch == 0) reinterpret_cast<unsigned char*>(sm.nan_blocks[buf])[key] = (unsigned char)bits;
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = w * 32 + i * 8 + (lane >> 2);
-              const uint32_t s2 = e4m3x2_to_half2(sc[i]), s_lo = __byte_perm(s2, 0, 0x1010), s_hi = __byte_perm(s2, 0, 0x3232);
-              unsigned char* row = op + key * 128;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                // word kk = k ^ swap of the four; the two orders differ by exchanging words (0, 2) and (1, 3)
-                const uint32_t c0 = k == 0 ? code[i].x : k == 1 ? code[i].y : k == 2 ? code[i].z : code[i].w;
-                const uint32_t c1 = k == 0 ? code[i].z : k == 1 ? code[i].w : k == 2 ? code[i].x : code[i].y;
-                const uint32_t c = swap ? c1 : c0;
-                const int kk = k ^ swap;
-                const uint32_t s = (kk & 2) ? s_hi : s_lo;
-                uint32_t h[4];
-                e2m1x8_to_half2(c, h);
-                *reinterpret_cast<uint4*>(row + ((((ch & 1) * 4 + kk) ^ (key & 7)) << 4)) =
-                    make_uint4(mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
-              }
-            }
-            fence_async_proxy();                         // for the tensor core's reads
+          for (int i = 0; i < 4; ++i) {
+            const int key = w * 32 + i * 8 + kr, pi = key >> a.page_log2, r = key & (page - 1);
+            const unsigned char* blk = raw + pi * page * kKv4Entry;
+            code[i] = *reinterpret_cast<const uint4*>(blk + r * 64 + ch * 16);
+            sc[i] = *reinterpret_cast<const unsigned short*>(blk + page * 64 + r * 8 + ch * 2);
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(which ? &sm.v_full[buf] : &sm.k_full[buf]);
         }
-        if (lane == 0) mbar_arrive(&sm.raw_empty[st]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.raw_empty[which][st]);  // (the codes are in registers)
+        // the operand buffer is free when the product two tiles back has read it (that of a K tile is announced by its logits)
+        if (it >= 2 && ok) {
+          const uint32_t b2 = (it - 2) % kBufs;
+          ok = which ? mbar_wait(&sm.v_empty[buf], ((it >> 1) - 1) & 1u) : mbar_wait(&sm.s_full[b2], ((it - 2) / kBufs) & 1u);
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok) {
+          if (which && tail) {
+            // Values nobody reads get a scale of zero (0 x NaN), and so does a NaN that some nodes read: the softmax warps, which know
+            // who does, hear of it by a bit per block.
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = w * 32 + i * 8 + kr, slot = pos0 + key - sg.ctx;
+              uint32_t bits = 0;
+              if (slot >= 0) {
+                const bool live = slot < a.Ns && ((__ldg(usedw + (slot >> 5)) >> (slot & 31)) & 1u);
+                const bool n0 = (sc[i] & 0x7Fu) == 0x7Fu, n1 = (sc[i] & 0x7F00u) == 0x7F00u;
+                if (live) bits = ((uint32_t)n0 | (uint32_t)n1 << 1) << (2 * ch);
+                if (!live) sc[i] = 0;
+                if (n0) sc[i] &= 0xFF00u;
+                if (n1) sc[i] &= 0x00FFu;
+              }
+              // the key's four lanes: two in this group of four, two in the group of the key two further
+              bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
+              bits |= __shfl_sync(0xffffffffu, bits, (lane ^ 2) ^ 8);
+              if (ch == 0) reinterpret_cast<unsigned char*>(sm.nan_blocks[buf])[key] = (unsigned char)bits;
+            }
+          }
+          unsigned char* op = smem + (which ? kOffV : kOffK) + buf * kOpBytes + (ch >> 1) * kHalfBytes;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = w * 32 + i * 8 + kr;
+            const uint32_t s2 = e4m3x2_to_half2(sc[i]), s_lo = __byte_perm(s2, 0, 0x1010), s_hi = __byte_perm(s2, 0, 0x3232);
+            const uint32_t words[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+            unsigned char* row = op + key * 128;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t s = k & 2 ? s_hi : s_lo;
+              uint32_t h[4];
+              e2m1x8_to_half2(words[k], h);
+              *reinterpret_cast<uint4*>(row + ((((ch & 1) * 4 + k) ^ (kr & 7)) << 4)) =
+                  make_uint4(mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
+            }
+          }
+          fence_async_proxy();                           // for the tensor core's reads
+        }
+        // tile t's S buffer is free when tile t - 3's probabilities have been used
+        if (!which && it >= 3 && ok) ok = mbar_wait(&sm.v_empty[(it - 3) & 1u], ((it - 3) >> 1) & 1u);
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&full[buf]);
+          if (which) mbar_arrive(&sm.pv_full[it % kBufs]);
+        }
       }
     }
     if (!ok) sm.timed_out = 1u;
   } else {
     // ---------------- softmax ----------------
-    // Warps w and w + 4 share the 32 rows of one lane quarter; the first takes keys 0..63 of every tile and output columns 0..63, the
-    // second the other halves.
+    // Warps w and w + 4 hold the 32 rows of one lane quarter; group `half` = warp / 4 takes the tiles of that parity, and at a segment's end
+    // the output columns [64 half, 64 half + 64).
     const int half = warp >> 2;
     const int row = 32 * (warp & 3) + lane;              // tensor-memory lane this warp may touch
     const uint32_t tmem_lane = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const int pair_bar = 1 + (warp & 3);                 // named barrier of the two warps of a lane quarter
+    const int pair_bar = 1 + (warp & 3);                 // named barriers of the two warps of a lane quarter: both wait ...
+    const int chain_bar = 5 + (warp & 3);                // ... (+ 4 parity) the reference maximum is that of the tile before
     const int GN = a.G * a.N;
-    // Query tile of a segment into tensor memory: this thread's half of its row, two f16 per column (zeros beyond the group); returns what
-    // takes the logits back to log2 units.  Called when the S products of the segment before have all completed (every thread
-    // awaited their s_full phases): for the first segment at once, for the others before that segment's read-out.
+    // Query tile of a segment into shared memory: this thread's half of its row in f16 (zeros beyond the group); returns what takes the logits
+    // back to log2 units.  The S products of the segment before have all completed by then: each group has awaited its own tiles', and
+    // the first barrier below is behind the last tiles of both.
     auto store_q = [&](const Segment& g) {
       const int rgq = g.rt * kRows + row;
       const bool okq = rgq < GN;
@@ -346,9 +423,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       const float up = exp2i(e);
 #pragma unroll
       for (int c = 0; c < 32; ++c) qr[c] = pack_half2(__uint_as_float(qr[c] << 16) * up, __uint_as_float(qr[c] & 0xFFFF0000u) * up);
-      tmem_st32(tmem_lane + kColQ + half * 32, qr);
-      tmem_st_wait();
-      tc_fence_before();
+      unsigned char* qd = smem + kOffQ + half * kHalfBytes + row * 128;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(qd + ((c ^ (row & 7)) << 4)) = make_uint4(qr[4 * c], qr[4 * c + 1], qr[4 * c + 2], qr[4 * c + 3]);
+      fence_async_proxy();                               // for the tensor core's reads
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
       return a.scale_log2 * exp2i(-e);
@@ -377,95 +455,124 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       float m = -INFINITY, l = 0.f;                      // reference maximum (log2 units), this thread's part of the row sum
       uint32_t nan_cols = 0;                             // blocks of the output that a NaN value reaches
       for (int j = 0; j < sg.n; ++j, ++it) {
-        const uint32_t buf = it & 1u;
-        const int kpos0 = (sg.t0 + j) * kKeys + half * 64;     // first key of this thread's 64
-        const bool tail = (sg.t0 + j + 1) * kKeys > sg.ctx;    // uniform: the tile reaches past the committed context
-        unsigned long long vm = ~0ull;
-        if (tail) vm = visible64(visw, kpos0 - sg.ctx);
-        if (ok) ok = mbar_wait(&sm.s_full[buf], (it >> 1) & 1u);
+        const uint32_t buf = it & 1u, sb = it % kBufs;
+        if ((int)buf != half) continue;                  // the other group's tile
+        const int kpos0 = (sg.t0 + j) * kKeys;
+        const bool tail = kpos0 + kKeys > sg.ctx;        // uniform: the tile reaches past the committed context
+        if (ok) ok = mbar_wait(&sm.s_full[sb], (it / kBufs) & 1u);
         tc_fence_after();
         __syncwarp();
         if (warp_ok) {
-          uint32_t sr[64];
-          tmem_ld32(tmem_lane + buf * kKeys + half * 64, sr);
-          tmem_ld32(tmem_lane + buf * kKeys + half * 64 + 32, sr + 32);
-          tmem_ld_wait();
-          if (tail) {                                    // a masked logit is replaced, never computed with
+          const uint32_t s_col = tmem_lane + sb * kKeys;
+          unsigned long long vm[2] = {~0ull, ~0ull};
+          if (tail) { vm[0] = visible64(visw, kpos0 - sg.ctx); vm[1] = visible64(visw, kpos0 + 64 - sg.ctx); }
+          if (tail) {                                    // a masked logit is replaced before anything is computed with it
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {
+              uint32_t sr[16];
+              tmem_ld16(s_col + c * 16, sr);
+              tmem_ld_wait();
+              const uint32_t v = (uint32_t)(vm[c >> 2] >> (16 * (c & 3)));
 #pragma unroll
-            for (int e = 0; e < 64; ++e) sr[e] = ((vm >> e) & 1ull) ? sr[e] : 0xFF800000u;
+              for (int e = 0; e < 16; ++e) sr[e] = ((v >> e) & 1u) ? sr[e] : 0xFF800000u;
+              tmem_st16(s_col + c * 16, sr);
+            }
+            tmem_st_wait();
           }
-          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          // ---- the row's maximum
+          float mx2[2] = {-INFINITY, -INFINITY};
+          uint32_t sr[2][16];                            // two sets of sixteen logits: one in use, one on its way
+          tmem_ld16(s_col, sr[0]);
 #pragma unroll
-          for (int e = 0; e < 64; ++e) mx4[e & 3] = fmaxf(mx4[e & 3], __uint_as_float(sr[e]));
-          float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * mul;
-          // Both threads of a row take the same decision: the reference moves when either half exceeds it by more than kLag.
-          if (pair_any(pair_bar, mx > m + kLag)) {
-            sm.xchg[half][row] = mx;
-            pair_sync(pair_bar);
-            mx = fmaxf(mx, sm.xchg[half ^ 1][row]);
-            pair_sync(pair_bar);                         // both have read before either writes there again
-            float corr = 1.f;
-            if (mx > m + kLag) { corr = m == -INFINITY ? 1.f : ex2(m - mx); m = mx; }
-            if (j > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
-              // O still takes the product of the tile before: wait for it, then scale this thread's columns
+          for (int c = 0; c < 8; ++c) {
+            tmem_ld_wait();
+            if (c < 7) tmem_ld16(s_col + (c + 1) * 16, sr[(c + 1) & 1]);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) mx2[(e >> 1) & 1] = max3(mx2[(e >> 1) & 1], __uint_as_float(sr[c & 1][e]), __uint_as_float(sr[c & 1][e + 1]));
+          }
+          const float mx = fmaxf(mx2[0], mx2[1]) * mul;
+          // ---- the reference maximum: that of the tile before, unless this tile exceeds it by more than kLag
+          float cur = -INFINITY;
+          if (j > 0) {
+            pair_sync(chain_bar + 4 * (int)(buf ^ 1u));
+            cur = sm.ref[row];
+          }
+          const float mnew = mx > cur + kLag ? mx : cur;
+          if (j + 1 < sg.n) {
+            sm.ref[row] = mnew;
+            pair_arrive(chain_bar + 4 * (int)buf);
+          }
+          if (__any_sync(0xffffffffu, mnew != m)) {      // some row's reference is not what this thread's sum goes by
+            if (j > 0 && __any_sync(0xffffffffu, mnew != cur && cur != -INFINITY)) {
+              // O still takes the product of the tile before: wait for it, then scale this row of it
+              const float corr = cur == -INFINITY ? 1.f : ex2(cur - mnew);
               if (ok) ok = mbar_wait(&sm.v_empty[(it - 1) & 1u], ((it - 1) >> 1) & 1u);
               tc_fence_after();
               __syncwarp();
 #pragma unroll 1
-              for (int c = 0; c < 64; c += 16) {
+              for (int c = 0; c < kDh; c += 16) {
                 uint32_t orr[16];
-                asm volatile(
-                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-                    : "=r"(orr[0]), "=r"(orr[1]), "=r"(orr[2]), "=r"(orr[3]), "=r"(orr[4]), "=r"(orr[5]), "=r"(orr[6]), "=r"(orr[7]),
-                      "=r"(orr[8]), "=r"(orr[9]), "=r"(orr[10]), "=r"(orr[11]), "=r"(orr[12]), "=r"(orr[13]), "=r"(orr[14]), "=r"(orr[15])
-                    : "r"(tmem_lane + kColO + half * 64 + c) : "memory");
+                tmem_ld16(tmem_lane + kColO + c, orr);
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) orr[e] = __float_as_uint(__uint_as_float(orr[e]) * corr);
-                asm volatile(
-                    "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n"
-                    ::"r"(tmem_lane + kColO + half * 64 + c), "r"(orr[0]), "r"(orr[1]), "r"(orr[2]), "r"(orr[3]), "r"(orr[4]), "r"(orr[5]), "r"(orr[6]),
-                      "r"(orr[7]), "r"(orr[8]), "r"(orr[9]), "r"(orr[10]), "r"(orr[11]), "r"(orr[12]), "r"(orr[13]), "r"(orr[14]), "r"(orr[15])
-                    : "memory");
+                tmem_st16(tmem_lane + kColO + c, orr);
               }
               tmem_st_wait();
-              l *= corr;
             }
+            if (m != mnew && m != -INFINITY) l *= ex2(m - mnew);
+            m = mnew;
           }
+          // ---- probabilities, sixteen keys at a time, the next sixteen logits on their way; over logits that have been read
           const float mu = m == -INFINITY ? 0.f : m - kLift;
-          uint32_t pk[32];
-          float ls4[4] = {0.f, 0.f, 0.f, 0.f};
+          const float2 mul2 = make_float2(mul, mul), mu2 = make_float2(-mu, -mu);
+          float2 ls[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
+          tmem_ld16(s_col, sr[0]);
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            const float p0 = ex2(fmaf(__uint_as_float(sr[c]), mul, -mu));
-            const float p1 = ex2(fmaf(__uint_as_float(sr[c + 1]), mul, -mu));
-            ls4[(c >> 1) & 3] += p0 + p1;
-            pk[c >> 1] = pack_half2(p0, p1);
+          for (int c = 0; c < 8; ++c) {
+            tmem_ld_wait();
+            if (c < 7) tmem_ld16(s_col + (c + 1) * 16, sr[(c + 1) & 1]);
+            const uint32_t* x = sr[c & 1];
+            uint32_t pk[8];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              const float2 y = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), mul2, mu2);
+              const float2 p = make_float2(ex2(y.x), ex2(y.y));
+              ls[(e >> 1) & 1] = add2(ls[(e >> 1) & 1], p);
+              pk[e >> 1] = pack_half2(p.x, p.y);
+            }
+            tmem_st8(s_col + c * 8, pk);
           }
-          l += (ls4[0] + ls4[1]) + (ls4[2] + ls4[3]);
-          tmem_st32(tmem_lane + buf * kKeys + half * 64, pk);
+          ls[0] = add2(ls[0], ls[1]);
+          l = ls[0].x + ls[0].y;
           tmem_st_wait();
           if (tail) {                                    // NaN values among the keys this row sees
             if (ok) ok = mbar_wait(&sm.v_full[buf], (it >> 1) & 1u);
             uint32_t any = 0;
 #pragma unroll 4
-            for (int c = 0; c < 16; ++c) any |= sm.nan_blocks[buf][half * 16 + c];
+            for (int c = 0; c < 32; ++c) any |= sm.nan_blocks[buf][c];
             if (any)
-              for (int e = 0; e < 64; ++e)
-                if ((vm >> e) & 1ull) nan_cols |= reinterpret_cast<const unsigned char*>(sm.nan_blocks[buf])[half * 64 + e];
+              for (int e = 0; e < kKeys; ++e)
+                if ((vm[e >> 6] >> (e & 63)) & 1ull) nan_cols |= reinterpret_cast<const unsigned char*>(sm.nan_blocks[buf])[e];
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.p_full[buf]);
+        if (lane == 0) mbar_arrive(&sm.pv_full[sb]);
       }
       // end of the segment.  First the next segment's queries (its logits then run under this read-out) ...
       have = work.next(&sgn);
       if (have && sgn.n > 0) mul_next = store_q(sgn);
-      // ... then the last O product, normalise and write the slot
+      // ... then the last O product, the two groups' sums, normalise and write the slot
       if (ok) ok = mbar_wait(&sm.v_empty[(it - 1) & 1u], ((it - 1) >> 1) & 1u);
       tc_fence_after();
       const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[nseg & 15u]) != 0;
+      const bool last = (int)((it - 1) & 1u) == half;    // this group had the last tile: its reference is the accumulator's
+      if (last) sm.ref[row] = m;
+      pair_sync(pair_bar);
+      const float mine = m;
+      m = sm.ref[row];
+      if (m != mine && mine != -INFINITY) l *= ex2(mine - m);
       sm.xchg[half][row] = l;
       pair_sync(pair_bar);
       const float lt = sm.xchg[0][row] + sm.xchg[1][row];
