@@ -37,7 +37,9 @@ namespace {
 // Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
 // The instruction count (about 420 per 16 keys and warp, of which 320 turn codes into f16) is near the time the bytes take.
 template <int NT> struct Small {
-  static constexpr int kWarps = NT == 1 ? 16 : 8;        // consumers; NT = 2 needs twice the registers
+  static constexpr int kWarps = NT == 1 ? 15 : 11;       // consumers; with the loader a multiple of four: 128 registers a thread, 168 for NT = 2
+  static constexpr int kSub = NT == 1 ? 2 : 1;           // groups of sixteen keys a warp takes at a time
+  static constexpr int kPieces = kKeys / 16 / kSub;      // pieces of a tile
   static constexpr int kStages = 8;
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kRedRow = 132;                    // floats per row of the reduction buffer: the stores of a half warp meet no bank twice
@@ -73,7 +75,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
   typename C::Ctl& sm = *reinterpret_cast<typename C::Ctl*>(smem + C::kOffCtl);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < C::kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 8); }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], C::kPieces); }
     sm.timed_out = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -92,13 +94,16 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
     // ---------------- loader ----------------
     const uint64_t policy = l2_evict_first_policy();
     while (work.next(&sg)) {
+      PageWalk walk(a, sg);
       for (int j = 0; j < sg.n; ++j, ++it) {
         const uint32_t st = it % C::kStages, use = it / C::kStages;
+        const bool wanted = walk.wanted(j);
+        const int pg = walk.take(j);
         if (use > 0 && ok) ok = mbar_wait(&sm.empty[st], (use - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (j == 0 && lane == 0) sm.bad_page[nseg & 15u] = 0;
-        load_tile(a, sg, sg.t0 + j, smem_u32(smem) + st * kTileBytes, &sm.full[st], &sm.bad_page[nseg & 15u], policy);
+        load_tile<true>(a, sg, wanted, pg, 0, smem_u32(smem) + st * kTileBytes, &sm.full[st], &sm.bad_page[nseg & 15u], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
@@ -109,14 +114,11 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
   } else {
     // ---------------- consumers ----------------
     const int g = lane >> 2, t = lane & 3;
-    const int grp = warp & 7;                            // keys [16 grp, 16 grp + 16) of a tile
     const int GN = a.G * a.N, page = 1 << a.page_log2;
-    const int c0 = grp * 16, pi = c0 >> a.page_log2, r0 = c0 & (page - 1);      // the group's page in the tile, first position in it
     const int kq = (g >> 1) + (g & 1) * 4;               // position of matrix row g among eight keys: lane t's value keys are t and t + 4
-    const uint32_t page_off = pi * page * 2 * kKv4Entry;
-    const uint32_t k_codes = page_off + (r0 + kq) * 64 + t * 16, k_scales = page_off + page * 64 + (r0 + kq) * 8 + t * 2;
-    const uint32_t v_codes = page_off + page * kKv4Entry + (r0 + t) * 64 + g * 8;
-    const uint32_t v_scales = page_off + page * (kKv4Entry + 64) + (r0 + t) * 8 + g;
+    // where this lane's parts of a group of sixteen keys lie, behind the group's page and its first position in it
+    const uint32_t k_codes = kq * 64 + t * 16, k_scales = page * 64 + kq * 8 + t * 2;
+    const uint32_t v_codes = page * kKv4Entry + t * 64 + g * 8, v_scales = page * (kKv4Entry + 64) + t * 8 + g;
     float* red = reinterpret_cast<float*>(smem + C::kOffRed);
     while (work.next(&sg)) {
       if (tid == 0) a.unit_slots[sg.unit] = make_int2(sg.slot0, sg.nslots);   // for the merge (same pair from every writer)
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
         }
       }
       const uint32_t* usedw = a.used + (size_t)sg.b * 8;
-      float o[NT][8][4], m[NT][2], l[NT][2];
+      float o[NT][8][4], m[NT][2], mu[NT][2], l[NT][2];       // mu: what is taken off the logits (a row without keys: 0)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -162,101 +164,129 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.f;
         m[nt][0] = m[nt][1] = -INFINITY;
-        l[nt][0] = l[nt][1] = 0.f;
+        mu[nt][0] = mu[nt][1] = l[nt][0] = l[nt][1] = 0.f;
       }
-      for (int j = 0; j < sg.n; ++j, ++it) {
-        if (C::kWarps == 16 && (int)(it & 1u) != warp >> 3) continue;           // the other eight warps' tile
-        const uint32_t st = it % C::kStages;
-        if (ok) ok = mbar_wait(&sm.full[st], (it / C::kStages) & 1u);
+      // the segment's pieces of 16 kSub keys are dealt out to the warps in turn
+      for (int gi = warp; gi < sg.n * C::kPieces; gi += C::kWarps) {
+        const uint32_t tt = it + gi / C::kPieces, st = tt % C::kStages;
+        const int first = (gi % C::kPieces) * 16 * C::kSub;
+        if (ok) ok = mbar_wait(&sm.full[st], (tt / C::kStages) & 1u);
         ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
-        const int pos0 = (sg.t0 + j) * kKeys + c0;       // the group's first position
+        const int pos0 = (sg.t0 + gi / C::kPieces) * kKeys + first;     // the piece's first position
         if (ok && pos0 < sg.ctx + a.Ns) {
-          const unsigned char* tile = smem + st * kTileBytes;
-          const bool tail = pos0 + 16 > sg.ctx;
-          // ---- S^T
-          float s[NT][4];
+          const bool tail = pos0 + 16 * C::kSub > sg.ctx;
+          const unsigned char *at_codes[C::kSub], *at_scales[C::kSub];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-          {
-            const uint4 ka = *reinterpret_cast<const uint4*>(tile + k_codes), kb = *reinterpret_cast<const uint4*>(tile + k_codes + 8 * 64);
-            const uint32_t sa = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(tile + k_scales));
-            const uint32_t sb = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(tile + k_scales + 8 * 8));
+          for (int u = 0; u < C::kSub; ++u) {            // a group of sixteen lies in one page
+            const int c0 = first + 16 * u, r0 = c0 & (page - 1);
+            const unsigned char* pg = smem + st * kTileBytes + (c0 >> a.page_log2) * (page * 2 * kKv4Entry);
+            at_codes[u] = pg + r0 * 64;
+            at_scales[u] = pg + r0 * 8;
+          }
+          // ---- S^T
+          float s[C::kSub][NT][4];
+#pragma unroll
+          for (int u = 0; u < C::kSub; ++u) {
+            float s2[NT][4];                             // two chains of four products each
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[u][nt][e] = s2[nt][e] = 0.f;
+            const uint4 ka = *reinterpret_cast<const uint4*>(at_codes[u] + k_codes), kb = *reinterpret_cast<const uint4*>(at_codes[u] + k_codes + 8 * 64);
+            const uint32_t sa = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(at_scales[u] + k_scales));
+            const uint32_t sb = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(at_scales[u] + k_scales + 8 * 8));
             const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+            const uint32_t fa[2] = {__byte_perm(sa, 0, 0x1010), __byte_perm(sa, 0, 0x3232)}, fb[2] = {__byte_perm(sb, 0, 0x1010), __byte_perm(sb, 0, 0x3232)};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {                // 32 t + 8 w ..: block 2 t for w < 2
               uint32_t ha[4], hb[4];
               e2m1x8_to_half2(wa[w], ha);
               e2m1x8_to_half2(wb[w], hb);
-              const uint32_t fa = __byte_perm(sa, 0, w < 2 ? 0x1010 : 0x3232), fb = __byte_perm(sb, 0, w < 2 ? 0x1010 : 0x3232);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                const uint32_t fr[4] = {mul_half2(ha[2 * k], fa), mul_half2(hb[2 * k], fb), mul_half2(ha[2 * k + 1], fa), mul_half2(hb[2 * k + 1], fb)};
+                const uint32_t fr[4] = {mul_half2(ha[2 * k], fa[w >> 1]), mul_half2(hb[2 * k], fb[w >> 1]), mul_half2(ha[2 * k + 1], fa[w >> 1]),
+                                        mul_half2(hb[2 * k + 1], fb[w >> 1])};
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], fr, qf[nt][4 * w + 2 * k], qf[nt][4 * w + 2 * k + 1]);
+                for (int nt = 0; nt < NT; ++nt) mma_f16(k ? s2[nt] : s[u][nt], fr, qf[nt][4 * w + 2 * k], qf[nt][4 * w + 2 * k + 1]);
               }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[u][nt][e] = (s[u][nt][e] + s2[nt][e]) * mul[nt][e & 1];
           }
-          // ---- softmax: s[nt] = (key kq: rows 2 t, 2 t + 1), (key 8 + kq: the same rows)
-          bool seen[NT][4];
+          // ---- softmax: s[u][nt] = (key kq of group u: rows 2 t, 2 t + 1), (key 8 + kq: the same rows).  A masked logit is replaced.
+          if (tail) {
+#pragma unroll
+            for (int u = 0; u < C::kSub; ++u)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (!slot_seen(vis[nt][e & 1], pos0 + 16 * u + kq + 8 * (e >> 1) - sg.ctx)) s[u][nt][e] = -INFINITY;
+          }
           bool over = false;
+          float top[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              s[nt][e] *= mul[nt][e & 1];
-              seen[nt][e] = true;
-              if (tail) seen[nt][e] = slot_seen(vis[nt][e & 1], pos0 + kq + 8 * (e >> 1) - sg.ctx);
-              over |= seen[nt][e] && s[nt][e] > m[nt][e & 1] + kLag;
+            for (int h = 0; h < 2; ++h) {
+              float x = fmaxf(s[0][nt][h], s[0][nt][2 + h]);
+#pragma unroll
+              for (int u = 1; u < C::kSub; ++u) x = fmaxf(x, fmaxf(s[u][nt][h], s[u][nt][2 + h]));
+              top[nt][h] = x;
+              over |= x > m[nt][h] + kLag;
             }
           if (__any_sync(0xffffffffu, over)) {           // some row's reference maximum has to move
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                float mx = fmaxf(seen[nt][h] ? s[nt][h] : -INFINITY, seen[nt][2 + h] ? s[nt][2 + h] : -INFINITY);
+                float mx = top[nt][h];
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
                 if (mx > m[nt][h] + kLag) {
                   const float corr = ex2(m[nt][h] - mx); // 0 the first time, when there is nothing to scale
                   m[nt][h] = mx;
+                  mu[nt][h] = mx - kLift;
                   l[nt][h] *= corr;
 #pragma unroll
                   for (int jj = 0; jj < 8; ++jj) { o[nt][jj][h] *= corr; o[nt][jj][2 + h] *= corr; }
                 }
               }
           }
-          uint32_t p0[NT], p1[NT];
+          uint32_t p0[C::kSub][NT], p1[C::kSub][NT];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float p[4];
+          for (int u = 0; u < C::kSub; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float mu = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1] - kLift;
-              p[e] = seen[nt][e] ? ex2(s[nt][e] - mu) : 0.f;
+            for (int nt = 0; nt < NT; ++nt) {
+              float p[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) p[e] = ex2(s[u][nt][e] - mu[nt][e & 1]);
+              l[nt][0] += p[0] + p[2];
+              l[nt][1] += p[1] + p[3];
+              p0[u][nt] = transpose8(pack_half2(p[0], p[1]));
+              p1[u][nt] = transpose8(pack_half2(p[2], p[3]));
             }
-            l[nt][0] += p[0] + p[2];
-            l[nt][1] += p[1] + p[3];
-            p0[nt] = transpose8(pack_half2(p[0], p[1]));
-            p1[nt] = transpose8(pack_half2(p[2], p[3]));
-          }
-          // ---- O^T: block g of keys t, t + 4 and t + 8, t + 12
-          uint32_t sc[2];
-          uint2 vc[4];
-          {
+          // ---- O^T: block g of keys t, t + 4 and t + 8, t + 12 of a group
+#pragma unroll
+          for (int u = 0; u < C::kSub; ++u) {
+            uint2 vc[4];
             uint32_t b4[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              vc[k] = *reinterpret_cast<const uint2*>(tile + v_codes + k * 4 * 64);
-              b4[k] = tile[v_scales + k * 4 * 8];
+              vc[k] = *reinterpret_cast<const uint2*>(at_codes[u] + v_codes + k * 4 * 64);
+              b4[k] = at_scales[u][v_scales + k * 4 * 8];
             }
             if (tail) {
               // Values nobody reads are left out of the product by a scale of zero (0 x NaN), and so is a NaN that some nodes read: it
               // turns block g of those nodes' outputs into NaN by hand.
+              const int slot0 = pos0 + 16 * u - sg.ctx;
               uint32_t nan = 0;                          // bit per key of the group
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                const int slot = pos0 + t + 4 * k - sg.ctx;
+                const int slot = slot0 + t + 4 * k;
                 if (slot < 0) continue;
                 const bool live = slot < a.Ns && ((__ldg(usedw + (slot >> 5)) >> (slot & 31)) & 1u);
                 if (live && (b4[k] & 0x7Fu) == 0x7Fu) nan |= 1u << (t + 4 * k);
@@ -265,41 +295,43 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
               if (__any_sync(0xffffffffu, nan != 0)) {
                 nan |= __shfl_xor_sync(0xffffffffu, nan, 1);
                 nan |= __shfl_xor_sync(0xffffffffu, nan, 2);     // block g, all sixteen keys
+                // the accumulators' rows of lane (g, t) are head elements of block g: its own mask
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                   for (int h = 0; h < 2; ++h) {
                     bool hit = false;
-                    for (int k = 0; k < 16; ++k) hit |= ((nan >> k) & 1u) && slot_seen(vis[nt][h], pos0 + k - sg.ctx);
+#pragma unroll 1
+                    for (int k = 0; k < 16; ++k) hit |= ((nan >> k) & 1u) && slot_seen(vis[nt][h], slot0 + k);
                     if (hit)
 #pragma unroll
                       for (int jj = 0; jj < 8; ++jj) o[nt][jj][h] = o[nt][jj][2 + h] = __int_as_float(0x7FC00000);
                   }
               }
             }
-            sc[0] = e4m3x2_to_half2(b4[0] | b4[1] << 8);
-            sc[1] = e4m3x2_to_half2(b4[2] | b4[3] << 8);
-          }
+            const uint32_t sc[2] = {e4m3x2_to_half2(b4[0] | b4[1] << 8), e4m3x2_to_half2(b4[2] | b4[3] << 8)};
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {                  // codes 8 w .. 8 w + 7 of the block
-            uint32_t ev[2][4], od[2][4];
+            for (int w = 0; w < 2; ++w) {                // codes 8 w .. 8 w + 7 of the block
+              uint32_t ev[2][4], od[2][4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint32_t x = w ? vc[2 * k].y : vc[2 * k].x, y = w ? vc[2 * k + 1].y : vc[2 * k + 1].x;
-              e2m1x8_to_half2((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), ev[k]);
-              e2m1x8_to_half2(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), od[k]);
-            }
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t x = w ? vc[2 * k].y : vc[2 * k].x, y = w ? vc[2 * k + 1].y : vc[2 * k + 1].x;
+                e2m1x8_to_half2((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), ev[k]);
+                e2m1x8_to_half2(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), od[k]);
+              }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t fr[4] = {mul_half2(ev[0][i], sc[0]), mul_half2(od[0][i], sc[0]), mul_half2(ev[1][i], sc[1]), mul_half2(od[1][i], sc[1])};
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t fr[4] = {mul_half2(ev[0][i], sc[0]), mul_half2(od[0][i], sc[0]), mul_half2(ev[1][i], sc[1]), mul_half2(od[1][i], sc[1])};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], fr, p0[nt], p1[nt]);
+                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], fr, p0[u][nt], p1[u][nt]);
+              }
             }
           }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.empty[st]);
       }
+      it += sg.n;
       // ---- the warps' parts meet: maxima and sums, then the outputs of eight rows at a time
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)

@@ -197,26 +197,43 @@ struct Work {
   }
 };
 
-// Stages one tile: a bulk copy per page that holds positions below ctx + Ns (the lanes of the loading warp take a page each).  A page
-// number out of range sets *bad_page, and nothing is copied for it.
-__device__ __forceinline__ void load_tile(const Kv4AttnArgs& a, const Segment& sg, int tile, uint32_t dst, unsigned long long* full, uint32_t* bad_page,
-                                          uint64_t policy) {
-  const int lane = threadIdx.x & 31;
-  const int page = 1 << a.page_log2, per_tile = kKeys >> a.page_log2;
-  const int pos = tile * kKeys + (lane << a.page_log2);
-  const bool mine = lane < per_tile && pos < sg.ctx + a.Ns;
-  int pg = -1;
-  if (mine) pg = __ldg(a.table + (size_t)sg.crow * a.max_pages + (pos >> a.page_log2));
-  const bool ok = mine && pg >= 0 && pg < a.n_pages;
-  const uint32_t bytes = page * 2 * kKv4Entry;
-  const unsigned good = __ballot_sync(0xffffffffu, ok);
-  const bool bad = __any_sync(0xffffffffu, mine && !ok);
+// The page numbers that a loading warp needs for a segment, a lane a page of the tile, asked for a tile ahead.
+struct PageWalk {
+  const int32_t* entries;
+  int n, per_tile, left, next;        // tiles, pages a tile; pages of the segment's row from its first one on; the number on its way
+  __device__ __forceinline__ PageWalk(const Kv4AttnArgs& a, const Segment& sg) {
+    const int lane = threadIdx.x & 31, first = (sg.t0 * kKeys) >> a.page_log2;
+    entries = a.table + (size_t)sg.crow * a.max_pages + first + lane;
+    n = sg.n;
+    per_tile = kKeys >> a.page_log2;
+    left = ((sg.ctx + a.Ns + (1 << a.page_log2) - 1) >> a.page_log2) - first - lane;
+    next = wanted(0) ? __ldg(entries) : -1;
+  }
+  // whether this lane has a page of tile j that holds positions below ctx + Ns
+  __device__ __forceinline__ bool wanted(int j) const { return (int)(threadIdx.x & 31) < per_tile && j < n && j * per_tile < left; }
+  __device__ __forceinline__ int take(int j) {
+    const int pg = next;
+    next = wanted(j + 1) ? __ldg(entries + (j + 1) * per_tile) : -1;
+    return pg;
+  }
+};
+
+// Stages one tile, or its keys (which = 0) or values (1) alone: a bulk copy per page.  A page number out of range sets *bad_page, and nothing
+// is copied for it.
+template <bool kBoth>
+__device__ __forceinline__ void load_tile(const Kv4AttnArgs& a, const Segment& sg, bool wanted, int pg, int which, uint32_t dst, unsigned long long* full,
+                                          uint32_t* bad_page, uint64_t policy) {
+  const int lane = threadIdx.x & 31, page = 1 << a.page_log2;
+  const bool good = wanted && pg >= 0 && pg < a.n_pages;
+  const uint32_t bytes = page * (kBoth ? 2 : 1) * kKv4Entry;
+  const unsigned loads = __ballot_sync(0xffffffffu, good);
+  const bool bad = __any_sync(0xffffffffu, wanted && !good);
   if (lane == 0) {
     if (bad) *reinterpret_cast<volatile uint32_t*>(bad_page) = 1;
-    mbar_expect_tx(full, __popc(good) * bytes);
+    mbar_expect_tx(full, __popc(loads) * bytes);
   }
   __syncwarp();
-  if (ok) bulk_load(dst + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, 0), bytes, full, policy);
+  if (good) bulk_load(dst + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, which), bytes, full, policy);
 }
 
 __device__ __forceinline__ bool slot_seen(const uint32_t* row, int s) {        // s: suffix slot; below 0: context

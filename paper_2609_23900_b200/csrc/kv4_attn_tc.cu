@@ -51,7 +51,7 @@ struct Ctl {
   unsigned long long q_full, o_free, drain[2];
   uint32_t tmem_base;
   uint32_t timed_out;
-  uint32_t bad_page[16];              // by segment number mod 16: the loader is never that far ahead
+  uint32_t bad_page[2][16];           // [keys' loader, values' loader], by segment number mod 16: the loader is never that far ahead
   SeqCache seq;
   float ref[kRows];                   // the rows' reference maxima
   float xchg[2][kRows];               // [group][row]: what the two threads of a row tell one another
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     sm.timed_out = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
-  if (tid < 16) sm.bad_page[tid] = 0;
+  if (tid < 32) sm.bad_page[0][tid] = 0;
   // The set-up above touches nothing of earlier kernels; everything below may.
   pdl_wait();
   pdl_trigger();
@@ -210,33 +210,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
   if (warp == kLoadWarp || warp == kLoadWarp + 1) {
     // ---------------- loaders: keys (which = 0) and values (1), a lane a page ----------------
     const uint64_t policy = l2_evict_first_policy();
-    const int page = 1 << a.page_log2, which = warp - kLoadWarp;
-    const uint32_t bytes = page * kKv4Entry;
+    const int which = warp - kLoadWarp;
     while (work.next(&sg)) {
-      const int32_t* entries = a.table + (size_t)sg.crow * a.max_pages + lane;
-      const int first_page = (sg.t0 * kKeys) >> a.page_log2, per_tile = kKeys >> a.page_log2, n_pg = (sg.ctx + a.Ns + page - 1) >> a.page_log2;
-      auto wants = [&](int j) { return lane < per_tile && j < sg.n && first_page + j * per_tile + lane < n_pg; };
-      int next = wants(0) ? __ldg(entries + first_page) : -1;          // page numbers are asked for a tile ahead
+      PageWalk walk(a, sg);
       for (int j = 0; j < sg.n; ++j, ++it) {
         const uint32_t st = it % kStages, use = it / kStages;
-        const bool wanted = wants(j);
-        const int pg = next;
-        next = wants(j + 1) ? __ldg(entries + first_page + (j + 1) * per_tile) : -1;
+        const bool wanted = walk.wanted(j);
+        const int pg = walk.take(j);
         if (use > 0 && ok) ok = mbar_wait(&sm.raw_empty[which][st], (use - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const bool good = wanted && pg >= 0 && pg < a.n_pages;
-        const unsigned loads = __ballot_sync(0xffffffffu, good);
-        const bool bad = __any_sync(0xffffffffu, wanted && !good);
-        if (lane == 0) {
-          if (j == 0 && !which) sm.bad_page[nseg & 15u] = 0;
-          if (bad && !which) *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[nseg & 15u]) = 1;
-          mbar_expect_tx(&sm.raw_full[which][st], __popc(loads) * bytes);
-        }
-        __syncwarp();
-        if (good)
-          bulk_load(sbase + kOffRaw + (which * kStages + st) * kRawBytes + lane * bytes, a.pages + kv4_block(a.Hkv, page, pg, sg.hkv, which), bytes,
-                    &sm.raw_full[which][st], policy);
+        if (j == 0 && lane == 0) sm.bad_page[which][nseg & 15u] = 0;
+        load_tile<false>(a, sg, wanted, pg, which, sbase + kOffRaw + (which * kStages + st) * kRawBytes, &sm.raw_full[which][st],
+                         &sm.bad_page[which][nseg & 15u], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
@@ -566,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       // ... then the last O product, the two groups' sums, normalise and write the slot
       if (ok) ok = mbar_wait(&sm.v_empty[(it - 1) & 1u], ((it - 1) >> 1) & 1u);
       tc_fence_after();
-      const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[nseg & 15u]) != 0;
+      const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;   // (both loaders see the same pages)
       const bool last = (int)((it - 1) & 1u) == half;    // this group had the last tile: its reference is the accumulator's
       if (last) sm.ref[row] = m;
       pair_sync(pair_bar);
