@@ -19,7 +19,8 @@ LIB = os.path.join(HERE, "liblumo_gdn.so")
 SOURCES = ["api.cu", "kernels.cu", "scan_gram.cu", "scan_solve.cu", "scan_stream.cu", "attn.cu", "kv_cache.cu", "accept.cu", "select.cu", "rope.cu", "kv4_io.cu", "kv4_attn.cu", "kv4_attn_tc.cu",
            "pages.cu", "api_kv4.cu", "tree_desc.cpp"]
 HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "call_order.h"), os.path.join(CSRC, "conv_split.h"), os.path.join(CSRC, "api_common.h"),
-           os.path.join(CSRC, "kv4.h"), os.path.join(CSRC, "kv4_attn.h"), os.path.join(ROOT, "include", "lumo_gdn.h")]
+           os.path.join(CSRC, "kv4.h"), os.path.join(CSRC, "kv4_attn.h"),
+           os.path.join(CSRC, "f32x2.h"), os.path.join(ROOT, "include", "lumo_gdn.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -408,8 +408,9 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
 
 // ---- combination ---------------------------------------------------------------------------
 // A thread takes one row of a unit and four columns; a slot holds its rows by groups of four columns, [column group][row][4], so a warp reads
-// 512 contiguous bytes.  Slots are taken in order (the result for a given decomposition is reproducible), weights 2^(lse - max lse).  A slot whose
-// log-sum-exp is +inf (no sum gives that) met a page that does not exist.
+// 512 contiguous bytes.  Slots are taken in order, eight to a flight of loads, against a running maximum: the
+// result for a given decomposition is reproducible.  A slot whose log-sum-exp is +inf (no sum gives that) met a page that
+// does not exist.
 __global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnArgs a) {
   constexpr int kBatch = 8;
   pdl_wait();          // launched as a programmatic dependent of the attention kernel: its slots are complete from here on
@@ -424,45 +425,54 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnArgs a) {
   const int hkv = rem / a.RT, rt = rem - hkv * a.RT, rg = rt * a.R + r;
   const int cx = a.ctx_len[b], cr = a.cache_row[b];
   const int2 sl = a.unit_slots[u];       // meaningless for a sequence that fails its check
-  const int st = seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos);
-  const float* lp = a.part_lse + (size_t)sl.x * a.R + (sl.y == 1 || rg >= a.G * a.N ? 0 : r);
-  float mx = -INFINITY;
-  if (st == LUMO_SEQ_OK)
-    for (int s = 0; s < sl.y; ++s) mx = fmaxf(mx, lp[(size_t)s * a.R]);
-  const bool bad = mx == INFINITY;
-  if (i < 32 && rem == 0 && a.status) {  // one warp a sequence
-    int late = 0;
+  const bool reports = i < 32 && rem == 0 && a.status;   // one warp a sequence
+  int late = 0;
+  if (reports)
     for (int c = i; c < a.C; c += 32) late |= a.cta_code[c];
+  const int st = seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos);
+  const bool row_ok = rg < a.G * a.N;
+  const int n = st == LUMO_SEQ_OK ? sl.y : 0;
+  const float* lp = a.part_lse + (size_t)sl.x * a.R + (sl.y == 1 || !row_ok ? 0 : r);
+  const float4* op = reinterpret_cast<const float4*>(a.part_o) + ((size_t)sl.x * 32 + cg) * a.R + r;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float mx = -INFINITY, den = 0.f;
+  bool bad = false;
+  for (int s0 = 0; s0 < n; s0 += kBatch) {
+    float4 v[kBatch];
+    float w[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const bool in = s0 + k < n;
+      w[k] = in ? lp[(size_t)(s0 + k) * a.R] : -INFINITY;
+      v[k] = in && n > 1 && row_ok ? op[(size_t)(s0 + k) * 32 * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float top = mx;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) { top = fmaxf(top, w[k]); bad |= w[k] == INFINITY; }
+    if (top == INFINITY) continue;
+    const float corr = mx == -INFINITY ? 1.f : ex2(mx - top);          // (nothing summed yet, or NaN alone)
+    den *= corr; acc.x *= corr; acc.y *= corr; acc.z *= corr; acc.w *= corr;
+    mx = top;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (w[k] == -INFINITY) continue;   // none, or a slot without keys for this row
+      const float x = mx == -INFINITY ? w[k] : ex2(w[k] - mx);         // (no maximum: every weight is a NaN)
+      den += x;
+      acc.x = fmaf(x, v[k].x, acc.x); acc.y = fmaf(x, v[k].y, acc.y);
+      acc.z = fmaf(x, v[k].z, acc.z); acc.w = fmaf(x, v[k].w, acc.w);
+    }
+  }
+  if (reports) {
     late = __any_sync(0xffffffffu, late);
     if (i == 0) a.status[b] = st != LUMO_SEQ_OK ? st : (late ? (int)LUMO_SEQ_TIMEOUT : (bad ? (int)LUMO_SEQ_BAD_PAGE : (int)LUMO_SEQ_OK));
   }
-  if (rg >= a.G * a.N) return;
+  if (!row_ok || n == 1) return;         // (a single segment: the attention kernel has written the outputs)
   const int hl = rg / a.N, node = rg - hl * a.N;
   const size_t row = ((size_t)b * a.N + node) * a.Hq + (size_t)hkv * a.G + hl;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float lse = 0.f;
-  if (st == LUMO_SEQ_OK && sl.y == 1) return;      // a single segment: the attention kernel has written the outputs
-  if (st == LUMO_SEQ_OK && !bad) {
-    const float4* op = reinterpret_cast<const float4*>(a.part_o) + ((size_t)sl.x * 32 + cg) * a.R + r;
-    float den = 0.f;
-    for (int s0 = 0; s0 < sl.y; s0 += kBatch) {
-      float4 v[kBatch];
-      float w[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const bool in = s0 + k < sl.y;
-        w[k] = in ? lp[(size_t)(s0 + k) * a.R] : -INFINITY;
-        v[k] = in ? op[(size_t)(s0 + k) * 32 * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        if (w[k] == -INFINITY) continue; // none, or a slot without keys for this row
-        const float x = mx == -INFINITY ? w[k] : ex2(w[k] - mx);       // (no maximum: every weight is a NaN)
-        den += x;
-        acc.x = fmaf(x, v[k].x, acc.x); acc.y = fmaf(x, v[k].y, acc.y);
-        acc.z = fmaf(x, v[k].z, acc.z); acc.w = fmaf(x, v[k].w, acc.w);
-      }
-    }
+  if (n == 0 || bad) {
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  } else {
     const float inv = row_inverse(den);
     acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
     lse = den == 0.f ? -INFINITY : (mx + log2f(den)) * kLn2;

@@ -21,6 +21,7 @@
 // 128 bytes a cycle; the two products take 1024 cycles, the exponentials 1024 on their own units, and the instructions of the softmax and
 // of the conversion about 1000 of the four schedulers.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the
 // memory.
+#include "f32x2.h"
 #include "kv4_attn.h"
 
 namespace lumo {
@@ -137,22 +138,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}// two fp32 operations in one instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n"
-      : "=l"(reinterpret_cast<unsigned long long&>(r))
-      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
-  return r;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 r;
-  asm("add.rn.f32x2 %0, %1, %2;\n"
-      : "=l"(reinterpret_cast<unsigned long long&>(r)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
-  return r;
-}
-
-// Visibility of 64 consecutive keys from suffix slot s0 on (negative: keys of the committed context, always visible), from a
+}// Visibility of 64 consecutive keys from suffix slot s0 on (negative: keys of the committed context, always visible), from a
 // node's 256-bit row over the suffix.
 __device__ __forceinline__ unsigned long long visible64(const uint32_t* row, int s0) {
   if (s0 >= kMaxAttnSlots) return 0ull;
@@ -511,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           }
           // ---- probabilities, sixteen keys at a time, the next sixteen logits on their way; over logits that have been read
           const float mu = m == -INFINITY ? 0.f : m - kLift;
-          const float2 mul2 = make_float2(mul, mul), mu2 = make_float2(-mu, -mu);
+          const float2 mulx2 = make_float2(mul, mul), mux2 = make_float2(-mu, -mu);
           float2 ls[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
           tmem_ld16(s_col, sr[0]);
 #pragma unroll
@@ -522,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
             uint32_t pk[8];
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-              const float2 y = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), mul2, mu2);
+              const float2 y = fma2(make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), mulx2, mux2);
               const float2 p = make_float2(ex2(y.x), ex2(y.y));
               ls[(e >> 1) & 1] = add2(ls[(e >> 1) & 1], p);
               pk[e >> 1] = pack_half2(p.x, p.y);

@@ -93,91 +93,104 @@ __global__ void __launch_bounds__(kThreads) kv4_write_kernel(const KL L, const K
   }
 }
 
-// Tokens listed one by one: entry of token t goes to position pos[t] of row row[t]; row -1 is passed over.  CTAs go through (token, round
-// of rows) pairs, two in flight.
+// Where the listed tokens of a CTA lie: offset of the page's first block, position in the page, whether there is such a place.
+constexpr int kMostTokens = 32;
+struct Places { long long page[kMostTokens]; int at[kMostTokens]; bool ok[kMostTokens]; };
+__device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& t, int t0, int n, bool writes, int32_t* status, Places& p) {
+  const int i = threadIdx.x;
+  if (i >= n) return;
+  const int tok = t0 + i;
+  const int row = t.row[tok], pos = t.pos[tok];
+  int pg;
+  const int st = kv4_token_check(s, row, pos, writes, &pg);
+  if (status) status[tok] = st;
+  p.ok[i] = st == LUMO_SEQ_OK && pg >= 0;
+  p.page[i] = (long long)kv4_block(s.Hkv, s.page, pg < 0 ? 0 : pg, 0, 0);
+  p.at[i] = pos & (s.page - 1);
+}
+
+// Tokens listed one by one: entry of token t goes to position pos[t] of row row[t]; row -1 is passed over.  A CTA takes `per` tokens: their
+// places are looked up once, by a thread each, while the first rows are on their way; four rows in flight per sixteen lanes.
 template <class KL>
-__global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const Kv4Shape s, const Kv4Tokens t) {
-  const int l = blockIdx.y;
+__global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const Kv4Shape s, const Kv4Tokens t, int per) {
+  constexpr int kFlight = 4;
+  __shared__ Places places;
+  const int l = blockIdx.y, t0 = blockIdx.x * per, n = min(per, t.T - t0);
   const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
-  const int rows = 2 * s.Hkv;
-  const long long items = (long long)t.T * rows; // one row each
-  const long long step = (long long)gridDim.x * kGroups;
+  const int rows = 2 * s.Hkv, items = n * rows;
   const float down_k = exp2i(-s.k_exp), down_v = exp2i(-s.v_exp);
-  struct Item { uint4 raw; unsigned char* blk; int at, which; bool ok; };
-  auto fetch = [&](long long it) {
-    Item x;
-    x.ok = it < items;
-    x.raw = make_uint4(0, 0, 0, 0);
-    x.blk = nullptr; x.at = 0; x.which = 0;
-    if (!x.ok) return x;
-    const int tok = (int)(it / rows), r = (int)(it - (long long)tok * rows);
-    x.which = r >= s.Hkv;
-    const int h = x.which ? r - s.Hkv : r;
-    x.raw = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(x.which ? L.vn[l] : L.kn[l]) + (long long)tok * s.kv_stride + h * 128) + lane16);
-    int pg;
-    const int st = kv4_token_check(s, t.row[tok], t.pos[tok], true, &pg);
-    if (r == 0 && lane16 == 0 && L.status[l]) L.status[l][tok] = st;
-    x.ok = st == LUMO_SEQ_OK && pg >= 0;
-    x.at = t.pos[tok] & (s.page - 1);
-    if (x.ok) x.blk = reinterpret_cast<unsigned char*>(L.pages[l]) + kv4_block(s.Hkv, s.page, pg, h, x.which);
-    return x;
+  uint4 raw[kFlight];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f) {
+      const int i = i0 + f * kGroups;
+      raw[f] = make_uint4(0, 0, 0, 0);
+      if (i >= items) continue;
+      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+      raw[f] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(which ? L.vn[l] : L.kn[l]) + (long long)(t0 + tl) * s.kv_stride + h * 128) + lane16);
+    }
   };
+  fetch(grp);
+  find_places(s, t, t0, n, true, L.status[l], places);
+  __syncthreads();
   // uniform over the CTA: the shuffles see whole warps
-  for (long long base = (long long)blockIdx.x * kGroups; base < items; base += 2 * step) {
-    const Item a = fetch(base + grp), c = fetch(base + step + grp);
-    store_row(a.blk + a.at * 64, a.blk + s.page * 64 + a.at * 8, a.raw, a.which ? down_v : down_k, lane16, a.ok);
-    store_row(c.blk + c.at * 64, c.blk + s.page * 64 + c.at * 8, c.raw, c.which ? down_v : down_k, lane16, c.ok);
+  for (int base = 0; base < items; base += kFlight * kGroups) {
+    if (base) fetch(base + grp);
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f) {
+      const int i = min(base + grp + f * kGroups, items - 1);
+      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+      unsigned char* blk = reinterpret_cast<unsigned char*>(L.pages[l]) + places.page[tl] + (size_t)(2 * h + which) * (s.page * kKv4Entry);
+      const int at = places.at[tl];
+      store_row(blk + at * 64, blk + s.page * 64 + at * 8, raw[f], which ? down_v : down_k, lane16, base + grp + f * kGroups < items && places.ok[tl]);
+    }
   }
 }
 
 // The way back: entries of the listed tokens in bf16 (exact); zeros for a token that fails its check or has row -1.
 __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const unsigned char* pages, const Kv4Shape s, const Kv4Tokens t, __nv_bfloat16* k_out,
-                                                            __nv_bfloat16* v_out, int32_t* status) {
+                                                            __nv_bfloat16* v_out, int32_t* status, int per) {
+  constexpr int kFlight = 8;
+  __shared__ Places places;
+  const int t0 = blockIdx.x * per, n = min(per, t.T - t0);
   const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
-  const int rows = 2 * s.Hkv;
-  const long long items = (long long)t.T * rows;
-  const long long step = (long long)gridDim.x * kGroups;
+  const int rows = 2 * s.Hkv, items = n * rows;
   const float up_k = exp2i(s.k_exp), up_v = exp2i(s.v_exp);
-  constexpr int kFlight = 4;
-  for (long long base = (long long)blockIdx.x * kGroups + grp; base < items; base += kFlight * step) {
+  find_places(s, t, t0, n, false, status, places);
+  __syncthreads();
+  for (int base = grp; base < items; base += kFlight * kGroups) {
     uint32_t codes[kFlight], sb[kFlight];
-    __nv_bfloat16* dst[kFlight];
-    float up[kFlight];
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const long long it = base + f * step;
-      dst[f] = nullptr; codes[f] = 0; sb[f] = 0; up[f] = 1.f;
-      if (it >= items) continue;
-      const int tok = (int)(it / rows), r = (int)(it - (long long)tok * rows);
-      const int which = r >= s.Hkv, h = which ? r - s.Hkv : r;
-      int pg;
-      const int st = kv4_token_check(s, t.row[tok], t.pos[tok], false, &pg);
-      if (r == 0 && lane16 == 0 && status) status[tok] = st;
-      dst[f] = (which ? v_out : k_out) + ((long long)tok * s.Hkv + h) * 128 + lane16 * 8;
-      up[f] = which ? up_v : up_k;
-      if (st != LUMO_SEQ_OK || pg < 0) continue;
-      const int at = t.pos[tok] & (s.page - 1);
-      const unsigned char* blk = pages + kv4_block(s.Hkv, s.page, pg, h, which);
+      const int i = base + f * kGroups;
+      codes[f] = 0; sb[f] = 0;
+      if (i >= items) continue;
+      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+      if (!places.ok[tl]) continue;
+      const unsigned char* blk = pages + places.page[tl] + (size_t)(2 * h + which) * (s.page * kKv4Entry);
+      const int at = places.at[tl];
       codes[f] = reinterpret_cast<const uint32_t*>(blk + at * 64)[lane16];
       sb[f] = blk[s.page * 64 + at * 8 + (lane16 >> 1)];
     }
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      if (!dst[f]) continue;
-      const float sc = e4m3_value(sb[f]) * up[f];
+      const int i = base + f * kGroups;
+      if (i >= items) continue;
+      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+      const float sc = e4m3_value(sb[f]) * (which ? up_v : up_k);
       uint32_t h2[4], w[4];
       e2m1x8_to_half2(codes[f], h2);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h2[i]));
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h2[k]));
         const __nv_bfloat162 o = __floats2bfloat162_rn(v.x * sc, v.y * sc);
-        w[i] = *reinterpret_cast<const uint32_t*>(&o);
+        w[k] = *reinterpret_cast<const uint32_t*>(&o);
       }
-      *reinterpret_cast<uint4*>(dst[f]) = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>((which ? v_out : k_out) + ((long long)(t0 + tl) * s.Hkv + h) * 128)[lane16] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -241,23 +254,26 @@ cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers
   return launch_kernel(kv4_write_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s);
 }
 
-// CTAs for `items` rows: enough to fill the GPU, no more than there is work for
-static unsigned row_ctas(long long items, int sms) {
-  const long long want = (items + kGroups - 1) / kGroups, most = 8LL * sms;
-  return (unsigned)(want < most ? want : most);
+// tokens a CTA takes: 128 rows' worth, fewer while the GPU is not covered
+static int tokens_per_cta(int T, int Hkv, int sms) {
+  int per = 128 / (2 * Hkv);
+  per = per < 1 ? 1 : (per > kMostTokens ? kMostTokens : per);
+  while (per > 1 && (T + per - 1) / per < 2 * sms) per /= 2;
+  return per;
 }
 
 cudaError_t launch_kv4_append(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const Kv4Tokens& t, int sms, bool pdl, cudaStream_t st) {
-  const dim3 grid(row_ctas((long long)t.T * 2 * s.Hkv, sms), n_layers);
-  if (n_layers <= kFewLayers) return launch_kernel(kv4_append_kernel<FewKv4Layers>, grid, dim3(kThreads), 0, st, pdl, few_layers(L), s, t);
-  return launch_kernel(kv4_append_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s, t);
+  const int per = tokens_per_cta(t.T, s.Hkv, sms);
+  const dim3 grid((t.T + per - 1) / per, n_layers);
+  if (n_layers <= kFewLayers) return launch_kernel(kv4_append_kernel<FewKv4Layers>, grid, dim3(kThreads), 0, st, pdl, few_layers(L), s, t, per);
+  return launch_kernel(kv4_append_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s, t, per);
 }
 
 cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int32_t* status, int sms,
                             bool pdl, cudaStream_t st) {
-  const dim3 grid(row_ctas((long long)t.T * 2 * s.Hkv, sms));
-  return launch_kernel(kv4_read_kernel, grid, dim3(kThreads), 0, st, pdl, reinterpret_cast<const unsigned char*>(pages), s, t,
-                       reinterpret_cast<__nv_bfloat16*>(k_out), reinterpret_cast<__nv_bfloat16*>(v_out), status);
+  const int per = tokens_per_cta(t.T, s.Hkv, sms);
+  return launch_kernel(kv4_read_kernel, dim3((t.T + per - 1) / per), dim3(kThreads), 0, st, pdl, reinterpret_cast<const unsigned char*>(pages), s, t,
+                       reinterpret_cast<__nv_bfloat16*>(k_out), reinterpret_cast<__nv_bfloat16*>(v_out), status, per);
 }
 
 cudaError_t launch_kv4_publish(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const int32_t* accepted, const int32_t* len, int lmax,

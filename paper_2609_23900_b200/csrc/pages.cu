@@ -171,9 +171,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_reserve_kernel(const Pa
 // once, in the place of the first entry that released it; the entries count in the order of the list, and the last one is stored first,
 // so that pages taken by one call and given back by another come off the list in the same order again.
 __global__ void __launch_bounds__(kPlanThreads, 1) pages_free_kernel(const PageTableDev t, const int32_t* rows, const int32_t* keep, int n, int32_t* status) {
-  __shared__ int first_of[kMaxPageRows + 1];                      // number of the row's first entry; beyond the last row: all
-  __shared__ int2 row_of[kMaxPageRows];                           // row, its first released page
-  const int i = threadIdx.x;
+  constexpr int kWarps = kPlanThreads / 32, kFlight = 4;          // a warp goes through its rows 128 entries at a time
+  __shared__ int4 row_of[kMaxPageRows];                           // row, its first released page, one behind the last, number of its first entry
+  __shared__ int given_of[kMaxPageRows];                          // pages the row gives back
+  const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
   const WorkView w(t);
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
@@ -189,58 +190,78 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_free_kernel(const PageT
   if (status && i < n) status[i] = st;
   unsigned long long all;
   const int before = (int)block_scan((unsigned long long)(row >= 0 ? have - left : 0), &all);
-  const int entries = (int)all;
-  if (i < kMaxPageRows) { first_of[i] = before; row_of[i] = make_int2(row < 0 ? 0 : row, left); }
-  if (i == 0) first_of[kMaxPageRows] = entries;
+  if (i < kMaxPageRows) { row_of[i] = row >= 0 ? make_int4(row, left, have, before) : make_int4(0, 0, 0, 0); given_of[i] = 0; }
   if (row >= 0) t.row_pages[row] = left;
   __syncthreads();
-  // table entry number e: the row whose entries hold it, by bisection
-  auto place = [&](int e) {
-    int lo = 0, hi = kMaxPageRows - 1;                            // the last row that starts at or before e
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (first_of[mid] <= e) lo = mid; else hi = mid - 1;
+  // f(place in the table, page or -1, number of the entry, whether there is one) for the entries of a row, in order, whole warps at a time
+  auto walk = [&](int r, auto f) {
+    const int4 g = row_of[r];
+    int32_t* mine = t.table + (size_t)g.x * t.max_pages;
+    for (int k0 = g.y; k0 < g.z; k0 += 32 * kFlight) {
+      int pg[kFlight];
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) {
+        const int k = k0 + 32 * q + lane;
+        pg[q] = k < g.z ? mine[k] : -1;
+        if (pg[q] < 0 || pg[q] >= t.n_pages) pg[q] = -1;          // (an entry that names no page releases none)
+      }
+      f(mine, k0, pg, g);
     }
-    return (size_t)row_of[lo].x * t.max_pages + row_of[lo].y + (e - first_of[lo]);
   };
-  auto page_at = [&](size_t at) {
-    const int pg = t.table[at];
-    return pg >= 0 && pg < t.n_pages ? pg : -1;                   // (an entry that names no page releases none)
+  for (int r = warp; r < n; r += kWarps)
+    walk(r, [&](int32_t*, int, const int* pg, const int4&) {
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q)
+        if (pg[q] >= 0) __stcg(&w.count[pg[q]], INT_MAX);
+    });
+  __syncthreads();
+  for (int r = warp; r < n; r += kWarps)
+    walk(r, [&](int32_t*, int k0, const int* pg, const int4& g) {
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q)
+        if (pg[q] >= 0) { atomicMin(&w.count[pg[q]], g.w + k0 + 32 * q + lane - g.y); atomicSub(&t.refs[pg[q]], 1); }
+    });
+  __syncthreads();
+  // an entry gives its page back when nobody holds the page any longer and it is the first that released it
+  auto gives = [&](const int* pg, int k0, const int4& g, bool* out) {
+    int ref[kFlight], first[kFlight];
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) { ref[q] = pg[q] >= 0 ? __ldcg(&t.refs[pg[q]]) : 1; first[q] = pg[q] >= 0 ? __ldcg(&w.count[pg[q]]) : -1; }
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) out[q] = ref[q] <= 0 && first[q] == g.w + k0 + 32 * q + lane - g.y;
   };
-  for (int e = i; e < entries; e += kPlanThreads) {
-    const int pg = page_at(place(e));
-    if (pg >= 0) __stcg(&w.count[pg], INT_MAX);
+  for (int r = warp; r < n; r += kWarps) {
+    int sum = 0;
+    walk(r, [&](int32_t*, int k0, const int* pg, const int4& g) {
+      bool gv[kFlight];
+      gives(pg, k0, g, gv);
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) sum += __popc(__ballot_sync(0xffffffffu, gv[q]));
+    });
+    if (lane == 0) given_of[r] = sum;
   }
   __syncthreads();
-  for (int e = i; e < entries; e += kPlanThreads) {
-    const int pg = page_at(place(e));
-    if (pg >= 0) { atomicMin(&w.count[pg], e); atomicSub(&t.refs[pg], 1); }
-  }
+  const int mine_given = i < n ? given_of[i] : 0;
+  const int rank0 = (int)block_scan((unsigned long long)mine_given, &all);
+  const int given = (int)all;
+  if (i < n) given_of[i] = rank0;                                 // now: pages given back by the rows before
+  const int free = min(max(*t.free_count, 0), t.n_pages - min(given, t.n_pages));
   __syncthreads();
-  auto gives = [&](int e, int pg) { return pg >= 0 && __ldcg(&t.refs[pg]) <= 0 && __ldcg(&w.count[pg]) == e; };
-  int back = 0;
-  for (int e = i; e < entries; e += kPlanThreads) back += gives(e, page_at(place(e)));
-  unsigned long long given;
-  block_scan((unsigned long long)back, &given);
-  const int free = min(max(*t.free_count, 0), t.n_pages - min((int)given, t.n_pages));
-  int rank = 0;                                                   // pages given back by the entries of earlier rounds
-  for (int e0 = 0; e0 < entries; e0 += kPlanThreads) {
-    const int e = e0 + i;
-    size_t at = 0;
-    int pg = -1;
-    if (e < entries) { at = place(e); pg = page_at(at); }
-    const bool g = e < entries && gives(e, pg);
-    unsigned long long here;
-    const int mine = (int)block_scan(g, &here);
-    if (g) {
-      t.free_list[free + (int)given - 1 - (rank + mine)] = pg;
-      t.refs[pg] = 0;
-    }
-    if (e < entries) t.table[at] = -1;
-    rank += (int)here;
+  for (int r = warp; r < n; r += kWarps) {
+    int rank = given_of[r];
+    walk(r, [&](int32_t* mine, int k0, const int* pg, const int4& g) {
+      bool gv[kFlight];
+      gives(pg, k0, g, gv);
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) {
+        const unsigned m = __ballot_sync(0xffffffffu, gv[q]);
+        if (gv[q]) t.free_list[free + given - 1 - (rank + __popc(m & ((1u << lane) - 1u)))] = pg[q];
+        rank += __popc(m);
+        if (k0 + 32 * q + lane < g.z) mine[k0 + 32 * q + lane] = -1;
+      }
+    });
   }
-  __syncthreads();
-  if (i == 0) *t.free_count = free + (int)given;
+  if (i == 0) *t.free_count = free + given;
 }
 
 // ---- fork ---------------------------------------------------------------------------------
