@@ -26,6 +26,11 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {
   const uint32_t h = e4m3x2_to_half2(byte & 0xFFu);
   return __low2float(*reinterpret_cast<const __half2*>(&h));
 }
+__device__ __forceinline__ float reciprocal(float x) {   // to about an ulp
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+  return r;
+}
 // two e2m1 codes (the first in the low half of the byte): nearest, ties to the even code, at most 6
 __device__ __forceinline__ uint32_t e2m1x2_of(float lo, float hi) {
   uint32_t r;

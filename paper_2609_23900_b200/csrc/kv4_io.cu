@@ -6,7 +6,8 @@
 //   s = 0: codes of zero; a block with a NaN: scale NaN, codes zero.
 //
 // The values are bf16, so a quotient that is not exactly on a border between two codes (or two scales) is at least 1/255 away from it,
-// relatively: the product with the scale's reciprocal, rounded to the 11 bits of f16, lands on a border exactly when the quotient does.
+// relatively: a product with a reciprocal that is off by a few ulp, rounded to 11 or 12 bits, lands on a border exactly when the quotient
+// does, and no division is needed.
 // Likewise c * s has at most six significant bits: reading back in bf16 is exact.
 //
 // All of it is data movement: sixteen lanes a row of 128 numbers, 16 bytes of bf16 a lane.
@@ -14,6 +15,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include "f32x2.h"
 #include "internal.h"
 #include "kv4.h"
 
@@ -35,16 +37,20 @@ __device__ __forceinline__ uint32_t quantise8(uint4 raw, float down, uint32_t* s
   for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   const bool nan = top > 0x7F800000u;
-  uint32_t sb = e4m3_of(__uint_as_float(top) * down / 6.f);
+  const float six = fminf(__uint_as_float(top) * down * (1.f / 6.f), 1024.f);          // (beyond 448 is 448; a NaN is seen to below)
+  const float wide = six * 4097.f;
+  uint32_t sb = e4m3_of(wide - (wide - six));    // to twelve bits first
   if (nan) sb = 0x7Fu;
   *scale_byte = sb;
   const float s = e4m3_value(sb);
-  const float r = nan || s == 0.f ? 0.f : down / s;
+  const float r = nan || s == 0.f ? 0.f : down * reciprocal(s);
+  const float2 r2 = make_float2(r, r);
   uint32_t codes = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // to f16's 11 bits first (above); a value of a block without scale becomes a zero of its sign
-    const __half2 q = __floats2half2_rn(__uint_as_float(w[i] << 16) * r, __uint_as_float(w[i] & 0xFFFF0000u) * r);
+    // to f16's 11 bits first; a value of a block without scale becomes a zero of its sign
+    const float2 x = mul2(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), r2);
+    const __half2 q = __floats2half2_rn(x.x, x.y);
     codes |= e2m1x2_of(__low2float(q), __high2float(q)) << (8 * i);
   }
   return nan ? 0u : codes;
@@ -122,29 +128,36 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const 
   const int rows = 2 * s.Hkv, items = n * rows;
   const float down_k = exp2i(-s.k_exp), down_v = exp2i(-s.v_exp);
   uint4 raw[kFlight];
-  auto fetch = [&](int i0) {
+  int where[kFlight];                            // token of the CTA << 16 | row (a head's keys, or Hkv + a head's values); -1: none
+  int tl = grp / rows, r = grp - tl * rows;      // the next one
+  const int step_t = kGroups / rows, step_r = kGroups - step_t * rows;
+  auto fetch = [&]() {
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const int i = i0 + f * kGroups;
       raw[f] = make_uint4(0, 0, 0, 0);
-      if (i >= items) continue;
-      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
-      raw[f] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(which ? L.vn[l] : L.kn[l]) + (long long)(t0 + tl) * s.kv_stride + h * 128) + lane16);
+      where[f] = tl < n ? tl << 16 | r : -1;
+      if (tl < n) {
+        const int which = r >= s.Hkv;
+        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(which ? L.vn[l] : L.kn[l]) + (long long)(t0 + tl) * s.kv_stride + (which ? r - s.Hkv : r) * 128;
+        raw[f] = __ldg(reinterpret_cast<const uint4*>(src) + lane16);
+      }
+      tl += step_t;
+      r += step_r;
+      if (r >= rows) { r -= rows; ++tl; }
     }
   };
-  fetch(grp);
+  fetch();
   find_places(s, t, t0, n, true, L.status[l], places);
   __syncthreads();
   // uniform over the CTA: the shuffles see whole warps
   for (int base = 0; base < items; base += kFlight * kGroups) {
-    if (base) fetch(base + grp);
+    if (base) fetch();
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const int i = min(base + grp + f * kGroups, items - 1);
-      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
-      unsigned char* blk = reinterpret_cast<unsigned char*>(L.pages[l]) + places.page[tl] + (size_t)(2 * h + which) * (s.page * kKv4Entry);
-      const int at = places.at[tl];
-      store_row(blk + at * 64, blk + s.page * 64 + at * 8, raw[f], which ? down_v : down_k, lane16, base + grp + f * kGroups < items && places.ok[tl]);
+      const int tok = where[f] < 0 ? 0 : where[f] >> 16, rr = where[f] & 0xFFFF, which = rr >= s.Hkv;
+      const int at = places.at[tok];
+      unsigned char* blk = reinterpret_cast<unsigned char*>(L.pages[l]) + places.page[tok] + (which ? 2 * (rr - s.Hkv) + 1 : 2 * rr) * (s.page * kKv4Entry);
+      store_row(blk + at * 64, blk + s.page * 64 + at * 8, raw[f], which ? down_v : down_k, lane16, where[f] >= 0 && places.ok[tok]);
     }
   }
 }
@@ -158,39 +171,44 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const unsigned char*
   const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
-  const int rows = 2 * s.Hkv, items = n * rows;
+  const int rows = 2 * s.Hkv;
   const float up_k = exp2i(s.k_exp), up_v = exp2i(s.v_exp);
   find_places(s, t, t0, n, false, status, places);
   __syncthreads();
-  for (int base = grp; base < items; base += kFlight * kGroups) {
+  int tl = grp / rows, r = grp - tl * rows;
+  const int step_t = kGroups / rows, step_r = kGroups - step_t * rows;
+  while (tl < n) {
     uint32_t codes[kFlight], sb[kFlight];
+    int where[kFlight];
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const int i = base + f * kGroups;
       codes[f] = 0; sb[f] = 0;
-      if (i >= items) continue;
-      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
-      if (!places.ok[tl]) continue;
-      const unsigned char* blk = pages + places.page[tl] + (size_t)(2 * h + which) * (s.page * kKv4Entry);
-      const int at = places.at[tl];
-      codes[f] = reinterpret_cast<const uint32_t*>(blk + at * 64)[lane16];
-      sb[f] = blk[s.page * 64 + at * 8 + (lane16 >> 1)];
+      where[f] = tl < n ? tl << 16 | r : -1;
+      if (tl < n && places.ok[tl]) {
+        const unsigned char* blk = pages + places.page[tl] + (r >= s.Hkv ? 2 * (r - s.Hkv) + 1 : 2 * r) * (s.page * kKv4Entry);
+        const int at = places.at[tl];
+        codes[f] = reinterpret_cast<const uint32_t*>(blk + at * 64)[lane16];
+        sb[f] = blk[s.page * 64 + at * 8 + (lane16 >> 1)];
+      }
+      tl += step_t;
+      r += step_r;
+      if (r >= rows) { r -= rows; ++tl; }
     }
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      const int i = base + f * kGroups;
-      if (i >= items) continue;
-      const int tl = i / rows, r = i - tl * rows, which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+      if (where[f] < 0) continue;
+      const int rr = where[f] & 0xFFFF, which = rr >= s.Hkv;
       const float sc = e4m3_value(sb[f]) * (which ? up_v : up_k);
       uint32_t h2[4], w[4];
       e2m1x8_to_half2(codes[f], h2);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h2[k]));
-        const __nv_bfloat162 o = __floats2bfloat162_rn(v.x * sc, v.y * sc);
+        const float2 v = mul2(__half22float2(*reinterpret_cast<const __half2*>(&h2[k])), make_float2(sc, sc));
+        const __nv_bfloat162 o = __floats2bfloat162_rn(v.x, v.y);
         w[k] = *reinterpret_cast<const uint32_t*>(&o);
       }
-      reinterpret_cast<uint4*>((which ? v_out : k_out) + ((long long)(t0 + tl) * s.Hkv + h) * 128)[lane16] = make_uint4(w[0], w[1], w[2], w[3]);
+      __nv_bfloat16* dst = (which ? v_out : k_out) + ((long long)(t0 + (where[f] >> 16)) * s.Hkv + (which ? rr - s.Hkv : rr)) * 128;
+      reinterpret_cast<uint4*>(dst)[lane16] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
