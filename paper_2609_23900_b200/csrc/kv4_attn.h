@@ -18,7 +18,7 @@ constexpr int kTileBytes = kKeys * 2 * kKv4Entry;   // 18432: keys and values, c
 constexpr int kSeqCache = 64;         // sequences whose context length, cache row and tile count are kept in shared memory
 constexpr float kLag = 8.f;           // the reference maximum moves when exceeded by more than this (log2 units)
 constexpr float kLift = 6.f;          // probabilities are held as 2^kLift times themselves: at most 2^14 in f16, and what f16 drops is below 2^-30
-constexpr uint32_t kSpinLimit = 1u << 24;
+constexpr uint32_t kSpinLimit = 1u << 22;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -14,7 +14,7 @@
 //   warps 18, 19 issuers: S = Q K^T into one of three S buffers (up to two tiles ahead of the probabilities, so that a group finds its next
 //                logits ready), and O += P V into an accumulator that stays in tensor memory for the whole segment.  The tensor core takes
 //                few instructions ahead, and a wait costs its issuer 150 cycles or more even when nothing is awaited (measured): so there
-//                are two, each with one wait and one commit a tile, and one issues while the other waits.  Q lies in shared memory: the
+//                are two, each with one commit and a wait or two a tile, and one issues while the other waits.  Q lies in shared memory: the
 //                tensor core reads it from there at the same rate (1024 cycles for both products either way, measured)
 //
 // What bounds it: shared memory carries 164 KB a tile (codes written and read, operands written and read by the tensor core), 1312 cycles at
@@ -46,9 +46,12 @@ constexpr int kOffRaw = 5 * kOpBytes;
 constexpr int kOffCtl = kOffRaw + 2 * kStages * kRawBytes;
 struct Ctl {
   unsigned long long raw_full[2][kStages], raw_empty[2][kStages];   // [keys, values]
-  unsigned long long k_full[2], v_full[2], v_empty[2];
+  unsigned long long k_full[2], v_full[2];
   unsigned long long s_full[kBufs];   // logits complete (and the K tile read)
   unsigned long long pv_full[kBufs];  // probabilities and values complete
+  // Product of P and V complete.  One per S buffer: whoever waits for tile t's here is itself needed for tile t + 3's, so no phase is missed
+  // (with two, the issuer of tile t's logits could come after tile t - 1's product, two phases late, and wait for ever).
+  unsigned long long o_done[kBufs];
   unsigned long long q_full, o_free, drain[2];
   uint32_t tmem_base;
   uint32_t timed_out;
@@ -168,9 +171,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     for (int s = 0; s < 2 * kStages; ++s) { mbar_init(&sm.raw_full[0][s], 1); mbar_init(&sm.raw_empty[0][s], kGroupWarps); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.k_full[s], kGroupWarps); mbar_init(&sm.v_full[s], kGroupWarps);
-      mbar_init(&sm.v_empty[s], 1);
     }
-    for (int s = 0; s < kBufs; ++s) { mbar_init(&sm.s_full[s], 1); mbar_init(&sm.pv_full[s], 2 * kGroupWarps); }
+    for (int s = 0; s < kBufs; ++s) { mbar_init(&sm.s_full[s], 1); mbar_init(&sm.pv_full[s], 2 * kGroupWarps); mbar_init(&sm.o_done[s], 1); }
     mbar_init(&sm.q_full, kSoftmaxWarps);
     mbar_init(&sm.o_free, kSoftmaxWarps);
     mbar_init(&sm.drain[0], 1);
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     if (!ok && lane == 0) sm.timed_out = 1u;
   } else if (warp == kIssueWarp) {
     // ---------------- issuer of S = Q K^T: both K-major, 128 rows of 128 B per dh half ----------------
-    // (K tile t is announced only when its S buffer is free too, see the conversion; whole warps run these loops, and one lane issues)
+    // (whole warps run these loops, and one lane issues)
     constexpr uint32_t id = umma_idesc(kRows, kKeys, 0);
     const uint64_t dq = umma_desc(sbase + kOffQ, 16, 1024), dk = umma_desc(sbase + kOffK, 16, 1024);
     while (work.next(&sg)) {
@@ -226,6 +228,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       if (ok) ok = mbar_wait(&sm.q_full, nseg & 1u);
       for (int j = 0; j < sg.n; ++j, ++it) {
         if (ok) ok = mbar_wait(&sm.k_full[it & 1u], (it >> 1) & 1u);
+        // tile t's S buffer is free when tile t - 3's probabilities have been used
+        if (it >= kBufs && ok) ok = mbar_wait(&sm.o_done[it % kBufs], (it / kBufs - 1) & 1u);
         tc_fence_after();
         const uint64_t kd = dk + (it & 1u) * (kOpBytes >> 4);
         const uint32_t d = tmem + (it % kBufs) * kKeys;
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         if (ok && elect_one()) {
 #pragma unroll
           for (int ks = 0; ks < kKeys / 16; ++ks) umma_ta(tmem + kColO, p + ks * 8, vd + ks * (2048 >> 4), id, (j == 0 && ks == 0) ? 0u : 1u);
-          umma_commit(&sm.v_empty[it & 1u]);
+          umma_commit(&sm.o_done[it % kBufs]);
         }
         __syncwarp();
       }
@@ -307,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         // the operand buffer is free when the product two tiles back has read it (that of a K tile is announced by its logits)
         if (it >= 2 && ok) {
           const uint32_t b2 = (it - 2) % kBufs;
-          ok = which ? mbar_wait(&sm.v_empty[buf], ((it >> 1) - 1) & 1u) : mbar_wait(&sm.s_full[b2], ((it - 2) / kBufs) & 1u);
+          ok = mbar_wait(which ? &sm.o_done[b2] : &sm.s_full[b2], ((it - 2) / kBufs) & 1u);
         }
         ok = __all_sync(0xffffffffu, ok);
         if (ok) {
@@ -350,8 +354,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           }
           fence_async_proxy();                           // for the tensor core's reads
         }
-        // tile t's S buffer is free when tile t - 3's probabilities have been used
-        if (!which && it >= 3 && ok) ok = mbar_wait(&sm.v_empty[(it - 3) & 1u], ((it - 3) >> 1) & 1u);
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&full[buf]);
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
             if (j > 0 && __any_sync(0xffffffffu, mnew != cur && cur != -INFINITY)) {
               // O still takes the product of the tile before: wait for it, then scale this row of it
               const float corr = cur == -INFINITY ? 1.f : ex2(cur - mnew);
-              if (ok) ok = mbar_wait(&sm.v_empty[(it - 1) & 1u], ((it - 1) >> 1) & 1u);
+              if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
               tc_fence_after();
               __syncwarp();
 #pragma unroll 1
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       have = work.next(&sgn);
       if (have && sgn.n > 0) mul_next = store_q(sgn);
       // ... then the last O product, the two groups' sums, normalise and write the slot
-      if (ok) ok = mbar_wait(&sm.v_empty[(it - 1) & 1u], ((it - 1) >> 1) & 1u);
+      if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
       tc_fence_after();
       const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;   // (both loaders see the same pages)
       const bool last = (int)((it - 1) & 1u) == half;    // this group had the last tile: its reference is the accumulator's
