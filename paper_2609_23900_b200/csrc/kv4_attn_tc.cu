@@ -46,12 +46,13 @@ constexpr int kOffRaw = 5 * kOpBytes;
 constexpr int kOffCtl = kOffRaw + 2 * kStages * kRawBytes;
 struct Ctl {
   unsigned long long raw_full[2][kStages], raw_empty[2][kStages];   // [keys, values]
-  unsigned long long k_full[2], v_full[2];
+  unsigned long long k_full[2];
   unsigned long long s_full[kBufs];   // logits complete (and the K tile read)
   unsigned long long pv_full[kBufs];  // probabilities and values complete
   // Product of P and V complete.  One per S buffer: whoever waits for tile t's here is itself needed for tile t + 3's, so no phase is missed
   // (with two, the issuer of tile t's logits could come after tile t - 1's product, two phases late, and wait for ever).
   unsigned long long o_done[kBufs];
+  unsigned long long v_full[kBufs];   // values (and nan_blocks) written, for softmax threads; three for the same reason
   unsigned long long q_full, o_free, drain[2];
   uint32_t tmem_base;
   uint32_t timed_out;
@@ -169,10 +170,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
   }
   if (tid == 0) {
     for (int s = 0; s < 2 * kStages; ++s) { mbar_init(&sm.raw_full[0][s], 1); mbar_init(&sm.raw_empty[0][s], kGroupWarps); }
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(&sm.k_full[s], kGroupWarps); mbar_init(&sm.v_full[s], kGroupWarps);
+    for (int s = 0; s < 2; ++s) mbar_init(&sm.k_full[s], kGroupWarps);
+    for (int s = 0; s < kBufs; ++s) {
+      mbar_init(&sm.s_full[s], 1); mbar_init(&sm.pv_full[s], 2 * kGroupWarps);
+      mbar_init(&sm.o_done[s], 1); mbar_init(&sm.v_full[s], kGroupWarps);
     }
-    for (int s = 0; s < kBufs; ++s) { mbar_init(&sm.s_full[s], 1); mbar_init(&sm.pv_full[s], 2 * kGroupWarps); mbar_init(&sm.o_done[s], 1); }
     mbar_init(&sm.q_full, kSoftmaxWarps);
     mbar_init(&sm.o_free, kSoftmaxWarps);
     mbar_init(&sm.drain[0], 1);
@@ -285,7 +287,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     // Lane (r, ch): codes [32 ch, 32 ch + 32) of a key, that is blocks 2 ch and 2 ch + 1.  Eight lanes (two keys, all of their codes) read 128
     // contiguous bytes; the lanes of the head's second half take the key two further, so that the eight write eight different 16-byte columns.
     const int ch = lane & 3, kr = (lane >> 2) ^ (ch & 2);
-    unsigned long long* full = which ? sm.v_full : sm.k_full;
     while (work.next(&sg)) {
       const uint32_t* usedw = a.used + (size_t)sg.b * 8;
       for (int j = 0; j < sg.n; ++j, ++it) {
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&full[buf]);
+          mbar_arrive(which ? &sm.v_full[it % kBufs] : &sm.k_full[buf]);
           if (which) mbar_arrive(&sm.pv_full[it % kBufs]);
         }
       }
@@ -521,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           l = ls[0].x + ls[0].y;
           tmem_st_wait();
           if (tail) {                                    // NaN values among the keys this row sees
-            if (ok) ok = mbar_wait(&sm.v_full[buf], (it >> 1) & 1u);
+            if (ok) ok = mbar_wait(&sm.v_full[sb], (it / kBufs) & 1u);
             uint32_t any = 0;
 #pragma unroll 4
             for (int c = 0; c < 32; ++c) any |= sm.nan_blocks[buf][c];
@@ -538,12 +539,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       have = work.next(&sgn);
       if (have && sgn.n > 0) mul_next = store_q(sgn);
       // ... then the last O product, the two groups' sums, normalise and write the slot
-      if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
-      tc_fence_after();
       const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;   // (both loaders see the same pages)
       const bool last = (int)((it - 1) & 1u) == half;    // this group had the last tile: its reference is the accumulator's
       if (last) sm.ref[row] = m;
       pair_sync(pair_bar);
+      // (behind the barrier: the last tile's logits are known to be there, hence the product three tiles before, whose phase this wait
+      // would otherwise take for the last one's)
+      if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
+      tc_fence_after();
       const float mine = m;
       m = sm.ref[row];
       if (m != mine && mine != -INFINITY) l *= ex2(mine - m);
