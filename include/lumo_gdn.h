@@ -494,7 +494,7 @@ typedef struct {
   int32_t out_dtype;        /* lumo_dtype of out */
   float* lse;               /* [B, N, Hq] fp32 or NULL */
   int32_t n_splits;         /* as in lumo_attn_args */
-  int32_t* status;          /* [B] (append: [T]); may be NULL */
+  int32_t* status;          /* [B], may be NULL; the calls that list tokens have an argument of their own and leave this alone */
   void* work;               /* attention: lumo_kv4_work_bytes bytes; calls that share it must not overlap */
   int64_t work_bytes;
 } lumo_kv4_args;
@@ -502,13 +502,14 @@ typedef struct {
 /* The tree's entries, quantised and written through the slot map.  A sequence is written whole or not at all. */
 int lumo_kv4_write_tree(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, void* stream);
 /* Tokens listed one by one (a prompt): entry of token t goes to position tok_pos[t] of row tok_row[t]; row -1 is passed over.  The
- * (row, position) pairs of a call must be distinct.  status [T].  ctx_len and cache_row are not read.  T * Hkv < 2^30. */
+ * (row, position) pairs of a call must be distinct.  status [T] (may be NULL) has a word per token, the same for all layers.  ctx_len
+ * and cache_row are not read.  T * Hkv < 2^30. */
 int lumo_kv4_append(lumo_ctx* ctx, const lumo_kv4_args* layers, int n_layers, int T, const int32_t* tok_row, const int32_t* tok_pos,
-                    void* stream);
+                    int32_t* status, void* stream);
 /* The listed tokens' entries of one layer as bf16 [T, Hkv, dh] (exact while 2^e keeps them in range); zeros for a token that is passed
- * over or refused.  status [T]. */
+ * over or refused.  status [T] or NULL. */
 int lumo_kv4_read(lumo_ctx* ctx, const lumo_kv4_args* layer, int T, const int32_t* tok_row, const int32_t* tok_pos, void* k_out, void* v_out,
-                  void* stream);
+                  int32_t* status, void* stream);
 /* Bytes of workspace lumo_kv4_attention needs for these trees, heads and splits (0 on a bad argument). */
 int64_t lumo_kv4_work_bytes(const lumo_ctx* ctx, const lumo_tree_desc* desc, int Hq, int Hkv, int n_splits);
 /* lumo_tree_attention over the 4-bit pages.  Codes times scales are exact in f16; probabilities enter the second product rounded to

@@ -175,8 +175,8 @@ _lib.lumo_qk_norm_rope.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POIN
 for _f in (_lib.lumo_kv4_write_tree, _lib.lumo_kv4_attention):
     _f.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_void_p]
 _lib.lumo_kv4_append.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
-                                 ctypes.c_void_p]
-_lib.lumo_kv4_read.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int] + [ctypes.c_void_p] * 5
+                                 ctypes.c_void_p, ctypes.c_void_p]
+_lib.lumo_kv4_read.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int] + [ctypes.c_void_p] * 6
 _lib.lumo_kv4_work_bytes.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_int]
 _lib.lumo_kv4_work_bytes.restype = ctypes.c_int64
 _lib.lumo_kv4_publish.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(_Kv4Args), ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
@@ -223,6 +223,15 @@ def _int32(**tensors):
     for name, t in tensors.items():
         if t is not None and t.dtype != torch.int32:
             raise ValueError(f"{name} must be int32")
+
+
+def _listed(first: torch.Tensor, **tensors) -> int:
+    """Length of a call's list: every int32 tensor of it has that many entries, ``status`` at least."""
+    n = first.numel()
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.int32 or (t.numel() < n if name == "status" else t.numel() != n)):
+            raise ValueError(f"{name} must be int32 with one entry per listed row or token")
+    return n
 
 
 def pages_work_ints(n_rows: int, n_pages: int) -> int:
@@ -399,16 +408,20 @@ class Context:
         arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
         self._check(_lib.lumo_kv4_write_tree(self._h, desc._h, arr, len(arr), _stream(stream)))
 
-    def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, stream=None):
-        """Entries of listed tokens (int32 rows and positions, [T]); a layer's ``status`` then has a word per token."""
+    def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
+        """Entries of listed tokens (int32 rows and positions, [T]); ``status``, if given, gets a word per token."""
         arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
-        _int32(tok_row=tok_row, tok_pos=tok_pos)
-        self._check(_lib.lumo_kv4_append(self._h, arr, len(arr), tok_row.numel(), _ptr(tok_row), _ptr(tok_pos), _stream(stream)))
+        T = _listed(tok_row, tok_row=tok_row, tok_pos=tok_pos, status=status)
+        self._check(_lib.lumo_kv4_append(self._h, arr, len(arr), T, _ptr(tok_row), _ptr(tok_pos), _ptr(status), _stream(stream)))
 
-    def kv4_read(self, layer: "Kv4Layer", tok_row: torch.Tensor, tok_pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, stream=None):
+    def kv4_read(self, layer: "Kv4Layer", tok_row: torch.Tensor, tok_pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
+                 status: Optional[torch.Tensor] = None, stream=None):
         """The listed tokens' entries as bf16 [T, Hkv, dh]."""
-        _int32(tok_row=tok_row, tok_pos=tok_pos)
-        self._check(_lib.lumo_kv4_read(self._h, layer.args, tok_row.numel(), _ptr(tok_row), _ptr(tok_pos), _ptr(k_out), _ptr(v_out),
+        T = _listed(tok_row, tok_row=tok_row, tok_pos=tok_pos, status=status)
+        for name, o in (("k_out", k_out), ("v_out", v_out)):
+            if o.dtype != torch.bfloat16 or not o.is_contiguous() or o.numel() < T * layer.args.Hkv * layer.args.dh:
+                raise ValueError(f"{name} must be contiguous bf16 [T, Hkv, dh]")
+        self._check(_lib.lumo_kv4_read(self._h, layer.args, T, _ptr(tok_row), _ptr(tok_pos), _ptr(k_out), _ptr(v_out), _ptr(status),
                                        _stream(stream)))
 
     def kv4_attention(self, desc: "TreeDesc", layers, stream=None):
@@ -427,23 +440,21 @@ class Context:
 
     def pages_fork(self, table: "PageTable", src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
         """Row dst[i], empty so far, shares the pages of row src[i]."""
-        _int32(src=src, dst=dst, status=status)
-        if src.numel() != dst.numel():
-            raise ValueError("src and dst must have the same length")
-        self._check(_lib.lumo_pages_fork(self._h, table.args, _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream(stream)))
+        n = _listed(src, src=src, dst=dst, status=status)
+        self._check(_lib.lumo_pages_fork(self._h, table.args, _ptr(src), _ptr(dst), n, _ptr(status), _stream(stream)))
 
     def pages_reserve(self, table: "PageTable", rows: torch.Tensor, start: torch.Tensor, end: Optional[torch.Tensor] = None, add: int = 0,
                       status: Optional[torch.Tensor] = None, stream=None):
         """Positions [start, end) (or [start, start + add)) of the rows made writable: shared pages copied, missing ones added."""
-        _int32(rows=rows, start=start, end=end, status=status)
-        self._check(_lib.lumo_pages_reserve(self._h, table.args, _ptr(rows), _ptr(start), _ptr(end), int(add), rows.numel(), _ptr(status),
+        n = _listed(rows, rows=rows, start=start, end=end, status=status)
+        self._check(_lib.lumo_pages_reserve(self._h, table.args, _ptr(rows), _ptr(start), _ptr(end), int(add), n, _ptr(status),
                                             _stream(stream)))
 
     def pages_free(self, table: "PageTable", rows: torch.Tensor, keep: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                    stream=None):
         """Pages behind the rows' first ``keep`` positions (all pages without it) given back."""
-        _int32(rows=rows, keep=keep, status=status)
-        self._check(_lib.lumo_pages_free(self._h, table.args, _ptr(rows), _ptr(keep), rows.numel(), _ptr(status), _stream(stream)))
+        n = _listed(rows, rows=rows, keep=keep, status=status)
+        self._check(_lib.lumo_pages_free(self._h, table.args, _ptr(rows), _ptr(keep), n, _ptr(status), _stream(stream)))
 
     def pages_compact(self, table: "PageTable", stream=None):
         """The pages in use moved to the lowest numbers, in all pools and tables."""
@@ -451,11 +462,9 @@ class Context:
 
     def rows_copy(self, blocks: "RowBlocks", src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
         """Row src[i] of every block copied to its row dst[i]."""
-        _int32(src=src, dst=dst, status=status)
-        if src.numel() != dst.numel():
-            raise ValueError("src and dst must have the same length")
+        n = _listed(src, src=src, dst=dst, status=status)
         self._check(_lib.lumo_rows_copy(self._h, blocks.ptrs, blocks.row_bytes, len(blocks.tensors), blocks.n_rows, _ptr(src), _ptr(dst),
-                                        src.numel(), _ptr(status), _stream(stream)))
+                                        n, _ptr(status), _stream(stream)))
 
 
 class TreeDesc:
@@ -631,6 +640,8 @@ class Kv4Layer:
             raise ValueError("pages must be a uint8 tensor [n_pages, Hkv, 2, page_size * 72]")
         if table.dim() != 2:
             raise ValueError("table must be [rows, max_pages]")
+        if refs is not None and refs.numel() != pages.shape[0]:
+            raise ValueError("refs must be [n_pages]")
         _int32(table=table, refs=refs, ctx_len=ctx_len, cache_row=cache_row, status=status)
         for name in ("q", "k_new", "v_new"):
             t = self.tensors[name]

@@ -178,7 +178,8 @@ int lumo_kv4_write_tree(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv
   return launched(ctx, e, CallOrder::kOther, "4-bit write launch");
 }
 
-int lumo_kv4_append(lumo_ctx* ctx, const lumo_kv4_args* layers, int n_layers, int T, const int32_t* tok_row, const int32_t* tok_pos, void* stream) {
+int lumo_kv4_append(lumo_ctx* ctx, const lumo_kv4_args* layers, int n_layers, int T, const int32_t* tok_row, const int32_t* tok_pos,
+                    int32_t* status, void* stream) {
   Kv4Shape s;
   int rc = prepare_kv4(ctx, nullptr, false, layers, n_layers, &s);
   if (rc == LUMO_OK) rc = check_new(ctx, layers, n_layers);
@@ -188,14 +189,14 @@ int lumo_kv4_append(lumo_ctx* ctx, const lumo_kv4_args* layers, int n_layers, in
   DeviceGuard g(ctx->device);
   cudaStream_t st = (cudaStream_t)stream;
   const Kv4Layers L = kv4_views(layers, n_layers);
-  const Kv4Tokens t = {T, tok_row, tok_pos};
+  const Kv4Tokens t = {T, tok_row, tok_pos, status};
   ctx->order.begin(ctx->device, stream);
   cudaError_t e = timed(ctx, LUMO_K_KV4_WRITE, st, [&] { return launch_kv4_append(L, s, n_layers, t, ctx->sm_count, ctx->overlap, st); });
   return launched(ctx, e, CallOrder::kOther, "4-bit append launch");
 }
 
 int lumo_kv4_read(lumo_ctx* ctx, const lumo_kv4_args* layer, int T, const int32_t* tok_row, const int32_t* tok_pos, void* k_out, void* v_out,
-                  void* stream) {
+                  int32_t* status, void* stream) {
   Kv4Shape s;
   int rc = prepare_kv4(ctx, nullptr, false, layer, 1, &s);
   if (rc == LUMO_OK) rc = check_tokens(ctx, s, T, tok_row, tok_pos);
@@ -204,10 +205,10 @@ int lumo_kv4_read(lumo_ctx* ctx, const lumo_kv4_args* layer, int T, const int32_
   if (const int host = launchable(ctx)) return host;
   DeviceGuard g(ctx->device);
   cudaStream_t st = (cudaStream_t)stream;
-  const Kv4Tokens t = {T, tok_row, tok_pos};
+  const Kv4Tokens t = {T, tok_row, tok_pos, status};
   ctx->order.begin(ctx->device, stream);
   cudaError_t e = timed(ctx, LUMO_K_KV4_READ, st, [&] {
-    return launch_kv4_read(layer->pages, s, t, k_out, v_out, layer->status, ctx->sm_count, ctx->overlap, st);
+    return launch_kv4_read(layer->pages, s, t, k_out, v_out, ctx->sm_count, ctx->overlap, st);
   });
   return launched(ctx, e, CallOrder::kOther, "4-bit read launch");
 }

@@ -402,11 +402,11 @@ inline FewKv4Layers few_layers(const Kv4Layers& L) {
   for (int i = 0; i < kFewLayers; ++i) { f.pages[i] = L.pages[i]; f.kn[i] = L.kn[i]; f.vn[i] = L.vn[i]; f.status[i] = L.status[i]; }
   return f;
 }
-// tokens listed one by one: T of them, rows and positions on the device
-struct Kv4Tokens { int T; const int32_t* row; const int32_t* pos; };
+// tokens listed one by one: T of them, rows and positions on the device; status may be null
+struct Kv4Tokens { int T; const int32_t* row; const int32_t* pos; int32_t* status; };
 cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, int sms, bool pdl, cudaStream_t st);
 cudaError_t launch_kv4_append(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const Kv4Tokens& t, int sms, bool pdl, cudaStream_t st);
-cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int32_t* status, int sms,
+cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int sms,
                             bool pdl, cudaStream_t st);
 cudaError_t launch_kv4_publish(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const int32_t* accepted, const int32_t* len, int lmax,
                                int32_t* ctx_len_out, bool pdl, cudaStream_t st);

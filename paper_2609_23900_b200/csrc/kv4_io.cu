@@ -102,14 +102,14 @@ __global__ void __launch_bounds__(kThreads) kv4_write_kernel(const KL L, const K
 // Where the listed tokens of a CTA lie: offset of the page's first block, position in the page, whether there is such a place.
 constexpr int kMostTokens = 32;
 struct Places { long long page[kMostTokens]; int at[kMostTokens]; bool ok[kMostTokens]; };
-__device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& t, int t0, int n, bool writes, int32_t* status, Places& p) {
+__device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& t, int t0, int n, bool writes, bool report, Places& p) {
   const int i = threadIdx.x;
   if (i >= n) return;
   const int tok = t0 + i;
   const int row = t.row[tok], pos = t.pos[tok];
   int pg;
   const int st = kv4_token_check(s, row, pos, writes, &pg);
-  if (status) status[tok] = st;
+  if (report && t.status) t.status[tok] = st;
   p.ok[i] = st == LUMO_SEQ_OK && pg >= 0;
   p.page[i] = (long long)kv4_block(s.Hkv, s.page, pg < 0 ? 0 : pg, 0, 0);
   p.at[i] = pos & (s.page - 1);
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const 
     }
   };
   fetch();
-  find_places(s, t, t0, n, true, L.status[l], places);
+  find_places(s, t, t0, n, true, l == 0, places);
   __syncthreads();
   // uniform over the CTA: the shuffles see whole warps
   for (int base = 0; base < items; base += kFlight * kGroups) {
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const 
 
 // The way back: entries of the listed tokens in bf16 (exact); zeros for a token that fails its check or has row -1.
 __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const unsigned char* pages, const Kv4Shape s, const Kv4Tokens t, __nv_bfloat16* k_out,
-                                                            __nv_bfloat16* v_out, int32_t* status, int per) {
+                                                            __nv_bfloat16* v_out, int per) {
   constexpr int kFlight = 8;
   __shared__ Places places;
   const int t0 = blockIdx.x * per, n = min(per, t.T - t0);
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const unsigned char*
   pdl_trigger();
   const int rows = 2 * s.Hkv;
   const float up_k = exp2i(s.k_exp), up_v = exp2i(s.v_exp);
-  find_places(s, t, t0, n, false, status, places);
+  find_places(s, t, t0, n, false, true, places);
   __syncthreads();
   int tl = grp / rows, r = grp - tl * rows;
   const int step_t = kGroups / rows, step_r = kGroups - step_t * rows;
@@ -287,11 +287,11 @@ cudaError_t launch_kv4_append(const Kv4Layers& L, const Kv4Shape& s, int n_layer
   return launch_kernel(kv4_append_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s, t, per);
 }
 
-cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int32_t* status, int sms,
+cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int sms,
                             bool pdl, cudaStream_t st) {
   const int per = tokens_per_cta(t.T, s.Hkv, sms);
   return launch_kernel(kv4_read_kernel, dim3((t.T + per - 1) / per), dim3(kThreads), 0, st, pdl, reinterpret_cast<const unsigned char*>(pages), s, t,
-                       reinterpret_cast<__nv_bfloat16*>(k_out), reinterpret_cast<__nv_bfloat16*>(v_out), status, per);
+                       reinterpret_cast<__nv_bfloat16*>(k_out), reinterpret_cast<__nv_bfloat16*>(v_out), per);
 }
 
 cudaError_t launch_kv4_publish(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const int32_t* accepted, const int32_t* len, int lmax,

@@ -68,8 +68,9 @@ def test_append_and_read_are_the_oracles_bit_for_bit(page, e):
         row[t], pos[t], want[t] = r, p, st
     row_d, pos_d = torch.from_numpy(row).cuda(), torch.from_numpy(pos).cuda()
     status = torch.full((T,), -1, dtype=torch.int32, device="cuda")
-    layer = binding.Kv4Layer(Hq=H, Hkv=H, pages=pages, table=table, page_size=page, k_new=k, v_new=v, k_exp=e[0], v_exp=e[1], status=status)
-    ctx().kv4_append([layer], row_d, pos_d)
+    own = torch.full((T,), -7, dtype=torch.int32, device="cuda")            # a layer's own words are for the calls on trees
+    layer = binding.Kv4Layer(Hq=H, Hkv=H, pages=pages, table=table, page_size=page, k_new=k, v_new=v, k_exp=e[0], v_exp=e[1], status=own)
+    ctx().kv4_append([layer], row_d, pos_d, status=status)
     torch.cuda.synchronize()
     assert status.tolist() == want.tolist()
     got, expect, tab = pages.cpu().numpy(), before.cpu().numpy(), table.cpu().numpy()
@@ -90,9 +91,9 @@ def test_append_and_read_are_the_oracles_bit_for_bit(page, e):
     assert np.array_equal(got, expect)
     kb, vb = torch.full((T, H, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, H, 128), 7.0, dtype=torch.bfloat16, device="cuda")
     status.fill_(-1)
-    ctx().kv4_read(layer, row_d, pos_d, kb, vb)
+    ctx().kv4_read(layer, row_d, pos_d, kb, vb, status=status)
     torch.cuda.synchronize()
-    assert status.tolist() == want.tolist()
+    assert status.tolist() == want.tolist() and set(own.tolist()) == {-7}
     for t in range(T):
         for h in range(H):
             for w, back in enumerate((kb, vb)):

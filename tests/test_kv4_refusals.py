@@ -105,8 +105,8 @@ def test_kv4_refusals(ctx):
         "attention": lambda *ls, d=desc, n=None: (lambda: lib.lumo_kv4_attention(ctx._h, d._h, layers(*ls), len(ls) if n is None else n, None)),
         "publish": lambda *ls, d=desc, n=None, lmax=4: (lambda: lib.lumo_kv4_publish(ctx._h, d._h, layers(*ls), len(ls) if n is None else n, PTR, PTR,
                                                                                       lmax, None, None)),
-        "append": lambda *ls, n=None, T=9: (lambda: lib.lumo_kv4_append(ctx._h, layers(*ls), len(ls) if n is None else n, T, PTR, PTR, None)),
-        "read": lambda *ls, T=9: (lambda: lib.lumo_kv4_read(ctx._h, layers(*ls), T, PTR, PTR, PTR, PTR, None)),
+        "append": lambda *ls, n=None, T=9: (lambda: lib.lumo_kv4_append(ctx._h, layers(*ls), len(ls) if n is None else n, T, PTR, PTR, None, None)),
+        "read": lambda *ls, T=9: (lambda: lib.lumo_kv4_read(ctx._h, layers(*ls), T, PTR, PTR, PTR, PTR, None, None)),
     }
     for name, call in calls.items():
         reaches_launch(ctx, call(kv()))
@@ -133,6 +133,34 @@ def test_kv4_refusals(ctx):
     for lmax in (0, 257):
         refused(ctx, calls["publish"](kv(), lmax=lmax), "lmax")
     assert ctx.kv4_work_bytes(desc, 8, 3) == 0 and ctx.kv4_work_bytes(desc, 8, 2, 33) == 0
+
+
+def test_lists_have_one_length(ctx, monkeypatch):
+    """Every word a call on a list writes or reads is inside the tensors given: refused before the library is asked."""
+    monkeypatch.setattr(B, "_ptr", lambda t: None if t is None else t.data_ptr())      # host tensors will do
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)    # noqa: E731
+    pages, t = torch.zeros(4, 2, 2, 16 * 72, dtype=torch.uint8), torch.zeros(2, 3, dtype=torch.int32)
+    layer = B.Kv4Layer(Hq=2, Hkv=2, pages=pages, table=t, page_size=16, status=i32(1))
+    out = torch.zeros(5, 2, 128, dtype=torch.bfloat16)
+    for kw in (dict(pos=i32(4)), dict(status=i32(4)), dict(status=torch.zeros(5)), dict(pos=i32(5).long())):
+        pos, st = kw.get("pos", i32(5)), kw.get("status")
+        with pytest.raises(ValueError):
+            ctx.kv4_append([layer], i32(5), pos, status=st)
+        with pytest.raises(ValueError):
+            ctx.kv4_read(layer, i32(5), pos, out, out, status=st)
+    for bad in (out[:4], out.float(), out.transpose(0, 1)):
+        with pytest.raises(ValueError):
+            ctx.kv4_read(layer, i32(5), i32(5), out, bad)
+    with pytest.raises(ValueError):
+        B.Kv4Layer(Hq=2, Hkv=2, pages=pages, table=t, page_size=16, refs=i32(3))
+    tab = B.PageTable(page_size=16, table=t, row_pages=i32(2), refs=i32(4), free_list=i32(4), free_count=i32(1), work=i32(B.pages_work_ints(2, 4)))
+    blocks = B.RowBlocks([torch.zeros(4, 8)])
+    for call in (lambda st: ctx.pages_fork(tab, i32(2), i32(2), status=st), lambda st: ctx.pages_free(tab, i32(2), status=st),
+                 lambda st: ctx.pages_reserve(tab, i32(2), i32(2), add=1, status=st), lambda st: ctx.rows_copy(blocks, i32(2), i32(2), status=st),
+                 lambda st: ctx.pages_fork(tab, i32(2), i32(1)), lambda st: ctx.rows_copy(blocks, i32(2), i32(3)),
+                 lambda st: ctx.pages_reserve(tab, i32(2), i32(2), end=i32(1)), lambda st: ctx.pages_free(tab, i32(2), keep=i32(1))):
+        with pytest.raises(ValueError):
+            call(i32(1))
 
 
 # ---- pages ----
