@@ -425,7 +425,7 @@ struct Kv4AttnArgs {
   float scale_log2;                                   // scale * log2(e) * 2^k_exp
   float v_mul;                                        // 2^v_exp
 };
-struct Kv4Plan { Kv4AttnArgs a; };
+struct Kv4Plan { Kv4AttnArgs a; int sms; };
 size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms);
 void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
               int n_splits, void* work, int sms, Kv4Plan* plan);

@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
   if (tid < 16) sm.bad_page[tid] = 0;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
-  fill_seq_cache(a, sm.seq);
+  if (warp == C::kWarps) C::W::set_up(a, sm.seq);
   __syncthreads();
   typename C::W work(a, sm.seq);
   Segment sg;
@@ -407,28 +407,34 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
 }
 
 // ---- combination ---------------------------------------------------------------------------
-// A thread takes one row of a unit and four columns; a slot holds its rows by groups of four columns, [column group][row][4], so a warp reads
-// 512 contiguous bytes.  Slots are taken in order, eight to a flight of loads, against a running maximum: the
-// result for a given decomposition is reproducible.  A slot whose log-sum-exp is +inf (no sum gives that) met a page that
-// does not exist.
-__global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnArgs a) {
-  constexpr int kBatch = 8;
-  pdl_wait();          // launched as a programmatic dependent of the attention kernel: its slots are complete from here on
-  pdl_trigger();
-  const int upb = a.Hkv * a.RT, per_unit = a.R * 32;
-  const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long uu = e / per_unit;
-  if (uu >= (long long)a.B * upb) return;
-  const int u = (int)uu, i = (int)(e - uu * per_unit);
-  const int cg = i / a.R, r = i - cg * a.R;
+// An entry is one row of a unit and four columns; a slot holds its rows by groups of four columns, [column group][row][4], so a warp reads 512
+// contiguous bytes.  kParts threads take an entry's slots in turn, each four to a flight of loads against a running maximum, and meet through
+// shared memory in order: the result for a given decomposition is reproducible.  A slot whose log-sum-exp is +inf (no sum gives that) met a
+// page that does not exist.  What it costs is the chain of loads (which slots, their weights and rows) and, with many rows, how many
+// threads an SM holds: hence the bound on registers.
+template <int kParts>
+__global__ void __launch_bounds__(256, 4) kv4_merge_kernel(const Kv4AttnArgs a, int r_log2) {
+  constexpr int kBatch = 4, kEntries = 256 / kParts;
+  __shared__ float4 acc_s[kParts > 1 ? 256 : 1];
+  __shared__ float2 stat_s[kParts > 1 ? 256 : 1];      // maximum, denominator
+  const int upb = a.Hkv * a.RT;
+  const int per_log2 = r_log2 + 5 - (kParts == 1 ? 8 : 6);               // CTAs per unit (R >= 8: at least one)
+  const int u = blockIdx.x >> per_log2, tid = threadIdx.x;
+  const int part = kParts == 1 ? 0 : tid / kEntries;
+  const int i = (blockIdx.x & ((1 << per_log2) - 1)) * kEntries + (tid & (kEntries - 1));
+  const int cg = i >> r_log2, r = i & ((1 << r_log2) - 1);
   const int b = u / upb, rem = u - b * upb;
   const int hkv = rem / a.RT, rt = rem - hkv * a.RT, rg = rt * a.R + r;
+  pdl_wait();          // launched as a programmatic dependent of the attention kernel: its slots are complete from here on
+  pdl_trigger();
   const int cx = a.ctx_len[b], cr = a.cache_row[b];
   const int2 sl = a.unit_slots[u];       // meaningless for a sequence that fails its check
-  const bool reports = i < 32 && rem == 0 && a.status;   // one warp a sequence
+  const bool reports = rem == 0 && i < 32 && part == 0 && a.status;      // one warp a sequence
   int late = 0;
-  if (reports)
+  if (reports) {
+#pragma unroll 5
     for (int c = i; c < a.C; c += 32) late |= a.cta_code[c];
+  }
   const int st = seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos);
   const bool row_ok = rg < a.G * a.N;
   const int n = st == LUMO_SEQ_OK ? sl.y : 0;
@@ -437,29 +443,50 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnArgs a) {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float mx = -INFINITY, den = 0.f;
   bool bad = false;
-  for (int s0 = 0; s0 < n; s0 += kBatch) {
-    float4 v[kBatch];
-    float w[kBatch];
+  if (n > 1 ? row_ok || reports : reports)
+    for (int s0 = part; s0 < n; s0 += kParts * kBatch) {
+      float4 v[kBatch];
+      float w[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const bool in = s0 + k < n;
-      w[k] = in ? lp[(size_t)(s0 + k) * a.R] : -INFINITY;
-      v[k] = in && n > 1 && row_ok ? op[(size_t)(s0 + k) * 32 * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < kBatch; ++k) {
+        const bool in = s0 + k * kParts < n;
+        w[k] = in ? lp[(size_t)(s0 + k * kParts) * a.R] : -INFINITY;
+        v[k] = in && n > 1 && row_ok ? op[(size_t)(s0 + k * kParts) * 32 * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float top = mx;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) { top = fmaxf(top, w[k]); bad |= w[k] == INFINITY; }
+      if (top == INFINITY) continue;
+      const float corr = mx == -INFINITY ? 1.f : ex2(mx - top);          // (nothing summed yet, or NaN alone)
+      den *= corr; acc.x *= corr; acc.y *= corr; acc.z *= corr; acc.w *= corr;
+      mx = top;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (w[k] == -INFINITY) continue;   // none, or a slot without keys for this row
+        const float x = mx == -INFINITY ? w[k] : ex2(w[k] - mx);         // (no maximum: every weight is a NaN)
+        den += x;
+        acc.x = fmaf(x, v[k].x, acc.x); acc.y = fmaf(x, v[k].y, acc.y);
+        acc.z = fmaf(x, v[k].z, acc.z); acc.w = fmaf(x, v[k].w, acc.w);
+      }
     }
-    float top = mx;
+  if constexpr (kParts > 1) {
+    acc_s[tid] = acc;
+    stat_s[tid] = make_float2(bad ? INFINITY : mx, den);
+    __syncthreads();
+    if (part) return;
+    float top = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) { top = fmaxf(top, w[k]); bad |= w[k] == INFINITY; }
-    if (top == INFINITY) continue;
-    const float corr = mx == -INFINITY ? 1.f : ex2(mx - top);          // (nothing summed yet, or NaN alone)
-    den *= corr; acc.x *= corr; acc.y *= corr; acc.z *= corr; acc.w *= corr;
+    for (int k = 0; k < kParts; ++k) { const float w = stat_s[k * kEntries + tid].x; bad |= w == INFINITY; top = fmaxf(top, w); }
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    den = 0.f;
     mx = top;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (w[k] == -INFINITY) continue;   // none, or a slot without keys for this row
-      const float x = mx == -INFINITY ? w[k] : ex2(w[k] - mx);         // (no maximum: every weight is a NaN)
-      den += x;
-      acc.x = fmaf(x, v[k].x, acc.x); acc.y = fmaf(x, v[k].y, acc.y);
-      acc.z = fmaf(x, v[k].z, acc.z); acc.w = fmaf(x, v[k].w, acc.w);
+    for (int k = 0; k < kParts; ++k) {
+      const float2 w = stat_s[k * kEntries + tid];
+      const float4 v = acc_s[k * kEntries + tid];
+      const float x = w.x == -INFINITY && w.y == 0.f ? 0.f : mx == -INFINITY ? 1.f : ex2(w.x - mx);       // (a part of NaN weights alone keeps its NaN)
+      den = fmaf(x, w.y, den);
+      acc.x = fmaf(x, v.x, acc.x); acc.y = fmaf(x, v.y, acc.y); acc.z = fmaf(x, v.z, acc.z); acc.w = fmaf(x, v.w, acc.w);
     }
   }
   if (reports) {
@@ -531,6 +558,7 @@ void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, cons
   const size_t units = (size_t)s.B * s.Hkv * a.RT, ctas = n_splits > 0 ? units * n_splits : (size_t)sms;
   const size_t slots = n_splits > 0 ? ctas : units + ctas;
   a.S = n_splits; a.C = (int)ctas; a.out_bf16 = out_bf16;
+  plan->sms = sms;
   a.scale_log2 = ldexpf(scale * kLog2e, s.k_exp);
   a.v_mul = ldexpf(1.f, s.v_exp);
   unsigned char* w = reinterpret_cast<unsigned char*>(work);
@@ -545,9 +573,14 @@ cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   return plan.a.R == 8 ? launch_small<1>(plan, pdl, st) : launch_small<2>(plan, pdl, st);
 }
 
+// Four threads an entry while all of their CTAs run at once: then the chain of flights is what the merge takes (a token at 4k: 3.7 us, 4.6
+// with one); one where four would come in several waves (4 x 8 nodes at 8k: 5.5 us, 7.4 with four).
 cudaError_t launch_kv4_merge(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
-  const long long threads = (long long)plan.a.B * plan.a.Hkv * plan.a.RT * plan.a.R * 32;
-  return launch_kernel(kv4_merge_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, pdl, plan.a);
+  const Kv4AttnArgs& a = plan.a;
+  const long long units = (long long)a.B * a.Hkv * a.RT;
+  const int r_log2 = a.R == 8 ? 3 : a.R == 16 ? 4 : 7;
+  if (units * a.R / 2 <= 4LL * plan.sms) return launch_kernel(kv4_merge_kernel<4>, dim3((unsigned)(units * a.R / 2)), dim3(256), 0, st, pdl, a, r_log2);
+  return launch_kernel(kv4_merge_kernel<1>, dim3((unsigned)(units * a.R / 8)), dim3(256), 0, st, pdl, a, r_log2);
 }
 
 }  // namespace lumo

@@ -86,7 +86,6 @@ __device__ __forceinline__ int query_exponent(uint32_t top) {
 // units are laid end to end on a line, each preceded by `cost` idle positions (the price of starting it, in tiles); CTA c owns the
 // positions [c * per, (c + 1) * per), works on the tiles among them, and the slot of a segment is u + c (strictly increasing along the line,
 // so unique).  Fixed mode (S partitions): CTA c owns partition c mod S of unit c / S, slot c.
-struct SeqCache { int ctx[kSeqCache], row[kSeqCache], nt[kSeqCache]; };
 struct Segment {
   int b, hkv, rt;     // unit
   int t0, n;          // first tile within the unit, tile count (n = 0 possible in fixed mode)
@@ -94,28 +93,32 @@ struct Segment {
   int unit, slot0, nslots;   // the unit, and the slots all its segments write (ascending along the key range)
   int ctx, crow;
 };
+struct WorkState {
+  int b, q;           // current sequence, unit within the sequence
+  int g, g_end;       // next position on the line, end of this CTA's share (the host bounds the line below 2^31)
+  int g_unit;         // position at which the current unit's stretch (idle prefix, then its tiles) starts
+  int nt;             // tiles per unit of the current sequence
+  int per;            // automatic mode: positions per CTA
+  int parts;          // partitions per unit when CTA c owns partition c mod parts of unit c / parts; 0: shares of the line
+  bool fixed_done;
+};
+// in shared memory: the first sequences, and what one warp has found out for all roles
+struct SeqCache {
+  int ctx[kSeqCache], row[kSeqCache], nt[kSeqCache];
+  WorkState work;     // behind the first segment
+  Segment first;
+  bool any;           // whether there is a first segment
+};
 
 __device__ __forceinline__ int seq_tiles(const Kv4AttnArgs& a, int cx, int cr) {
   return seq_check(cx, cr, a.Ns, a.n_rows, a.max_pos) == LUMO_SEQ_OK ? (cx + a.Ns + kKeys - 1) / kKeys : 0;
 }
-__device__ __forceinline__ void fill_seq_cache(const Kv4AttnArgs& a, SeqCache& s) {
-  if (threadIdx.x < kSeqCache && threadIdx.x < a.B) {
-    const int cx = a.ctx_len[threadIdx.x], cr = a.cache_row[threadIdx.x];
-    s.ctx[threadIdx.x] = cx; s.row[threadIdx.x] = cr; s.nt[threadIdx.x] = seq_tiles(a, cx, cr);
-  }
-}
 
 template <int kCost, int kMinTiles, int kSlack>
-struct Work {
+struct Work : WorkState {
   const Kv4AttnArgs& a;
   const SeqCache& sc;
-  int b = 0, q = 0;   // current sequence, unit within the sequence
-  int g = 0, g_end = 0;       // next position on the line, end of this CTA's share (the host bounds the line below 2^31)
-  int g_unit = 0;     // position at which the current unit's stretch (idle prefix, then its tiles) starts
-  int nt = 0;         // tiles per unit of the current sequence
-  int per = 1;        // automatic mode: positions per CTA
-  int parts;          // partitions per unit when CTA c owns partition c mod parts of unit c / parts; 0: shares of the line
-  bool fixed_done = false;
+  bool fresh = true;
 
   __device__ __forceinline__ int tiles_of(int bb, int* ctx, int* crow) const {
     if (bb < kSeqCache) { *ctx = sc.ctx[bb]; *crow = sc.row[bb]; return sc.nt[bb]; }
@@ -124,33 +127,81 @@ struct Work {
     return seq_tiles(a, *ctx, *crow);
   }
 
-  __device__ Work(const Kv4AttnArgs& args, const SeqCache& cache) : a(args), sc(cache), parts(args.S) {
-    if (parts > 0) return;
+  __device__ __forceinline__ Work(const Kv4AttnArgs& args, const SeqCache& cache) : WorkState(cache.work), a(args), sc(cache) {}
+
+  // Run by one warp, before the roles part: fills the cache, finds the CTA's share, a lane a sequence, and the share's first segment.  (By
+  // every warp for itself, sequence after sequence, this took 1700 cycles of each CTA's start; a copy of it takes a few dozen.)
+  static __device__ __forceinline__ void set_up(const Kv4AttnArgs& a, SeqCache& sc) {
+    const int lane = threadIdx.x & 31;
     const int upb = a.Hkv * a.RT;       // units per sequence
     int total = 0, most = 0, cx, cr;
-    for (int bb = 0; bb < a.B; ++bb) {
-      const int n = tiles_of(bb, &cx, &cr);
-      if (n > 0) total += (n + kCost) * upb;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const int bb = b0 + lane;
+      int n = 0;
+      if (bb < a.B) {
+        cx = a.ctx_len[bb];
+        cr = a.cache_row[bb];
+        n = seq_tiles(a, cx, cr);
+        if (bb < kSeqCache) { sc.ctx[bb] = cx; sc.row[bb] = cr; sc.nt[bb] = n; }
+      }
+      total += n > 0 ? (n + kCost) * upb : 0;
       most = max(most, n);
     }
-    per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
-    // Short contexts: when there is a CTA for every unit and no unit is much longer than an even share, units stay whole: nothing
-    // is cut, and with one segment per unit the outputs are final when they leave this kernel.
-    if (a.B * upb <= (int)gridDim.x && most <= per + kSlack) { parts = 1; return; }
-    if (per < kMinTiles) per = kMinTiles;
-    g = (int)blockIdx.x * per;
-    g_end = g + per < total ? g + per : total;
-    int acc = 0;                        // the unit whose stretch holds position g
-    for (b = 0; b < a.B; ++b) {
-      nt = tiles_of(b, &cx, &cr);
-      const int span = nt > 0 ? (nt + kCost) * upb : 0;
-      if (g < acc + span) { q = (g - acc) / (nt + kCost); g_unit = acc + q * (nt + kCost); break; }
-      acc += span;
+    total = __reduce_add_sync(0xffffffffu, total);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) sc.work = {0, 0, 0, 0, 0, 0, 1, a.S, false};
+    __syncwarp();
+    Work w(a, sc);
+    if (w.parts == 0) {
+      w.per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+      // Short contexts: when there is a CTA for every unit and no unit is much longer than an even share, units stay whole: nothing
+      // is cut, and with one segment per unit the outputs are final when they leave this kernel.
+      if (a.B * upb <= (int)gridDim.x && most <= w.per + kSlack) w.parts = 1;
     }
+    if (w.parts == 0) {
+      if (w.per < kMinTiles) w.per = kMinTiles;
+      w.g = (int)blockIdx.x * w.per;
+      w.g_end = w.g + w.per < total ? w.g + w.per : total;
+      int acc = 0;                      // the sequence whose units hold position g, and where they start
+      w.b = a.B;
+      for (int b0 = 0; b0 < a.B && w.g < w.g_end; b0 += 32) {
+        const int n = b0 + lane < a.B ? w.tiles_of(b0 + lane, &cx, &cr) : 0;
+        const int span = n > 0 ? (n + kCost) * upb : 0;
+        int upto = span;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const int x = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += x;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, w.g < acc + upto);
+        if (hit) {
+          const int at = __ffs(hit) - 1;
+          acc += __shfl_sync(0xffffffffu, upto - span, at);
+          w.nt = __shfl_sync(0xffffffffu, n, at);
+          w.b = b0 + at;
+          w.q = (w.g - acc) / (w.nt + kCost);
+          w.g_unit = acc + w.q * (w.nt + kCost);
+          break;
+        }
+        acc += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
+    Segment sg = {};
+    const bool any = w.advance(&sg);
+    if (lane == 0) { sc.work = w; sc.first = sg; sc.any = any; }
   }
 
   // next segment of this CTA; false when the share is exhausted
   __device__ __forceinline__ bool next(Segment* s) {
+    if (fresh) {
+      fresh = false;
+      *s = sc.first;
+      return sc.any;
+    }
+    return advance(s);
+  }
+
+  __device__ __forceinline__ bool advance(Segment* s) {
     const int upb = a.Hkv * a.RT;
     if (parts > 0) {
       if (fixed_done) return false;

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
   // The set-up above touches nothing of earlier kernels; everything below may.
   pdl_wait();
   pdl_trigger();
-  fill_seq_cache(a, sm.seq);
+  if (warp == 0) TcWork::set_up(a, sm.seq);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
