@@ -46,7 +46,9 @@ template <int NT> struct Small {
   static constexpr int kOffRed = kStages * kTileBytes;
   static constexpr int kOffCtl = kOffRed + kWarps * 8 * kRedRow * 4;
   struct Ctl {
-    unsigned long long full[kStages], empty[kStages];
+    // Two per stage, taken in turn: a warp may wait for a tile while the copies of the one before it in that stage are still on their way (it
+    // has pieces of every fourth tile or so, and copies may overtake one another), and would take that one's phase for its own.
+    unsigned long long full[2 * kStages], empty[kStages];
     SeqCache seq;
     float stat[kWarps][8 * NT][2];                       // a warp's reference maximum and sum of each row
     uint32_t timed_out;
@@ -75,7 +77,8 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
   typename C::Ctl& sm = *reinterpret_cast<typename C::Ctl*>(smem + C::kOffCtl);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < C::kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], C::kPieces); }
+    for (int s = 0; s < C::kStages; ++s) mbar_init(&sm.empty[s], C::kPieces);
+    for (int s = 0; s < 2 * C::kStages; ++s) mbar_init(&sm.full[s], 1);
     sm.timed_out = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
@@ -103,14 +106,14 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (j == 0 && lane == 0) sm.bad_page[nseg & 15u] = 0;
-        load_tile<true>(a, sg, wanted, pg, 0, smem_u32(smem) + st * kTileBytes, &sm.full[st], &sm.bad_page[nseg & 15u], policy);
+        load_tile<true>(a, sg, wanted, pg, 0, smem_u32(smem) + st * kTileBytes, &sm.full[it % (2 * C::kStages)], &sm.bad_page[nseg & 15u], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
     }
     if (!ok && lane == 0) sm.timed_out = 1;
-    // no copy may be on its way when the CTA leaves: the last use of every stage (complete already unless a wait ran out)
-    for (uint32_t s = 0; s < C::kStages && s < it; ++s) mbar_wait(&sm.full[s], (((it - 1 - s) / C::kStages)) & 1u);
+    // no copy may be on its way when the CTA leaves: the last use of every barrier (complete already unless a wait ran out)
+    for (uint32_t s = 0; s < 2 * C::kStages && s < it; ++s) mbar_wait(&sm.full[s], ((it - 1 - s) / (2 * C::kStages)) & 1u);
   } else {
     // ---------------- consumers ----------------
     const int g = lane >> 2, t = lane & 3;
@@ -170,7 +173,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
       for (int gi = warp; gi < sg.n * C::kPieces; gi += C::kWarps) {
         const uint32_t tt = it + gi / C::kPieces, st = tt % C::kStages;
         const int first = (gi % C::kPieces) * 16 * C::kSub;
-        if (ok) ok = mbar_wait(&sm.full[st], (tt / C::kStages) & 1u);
+        if (ok) ok = mbar_wait(&sm.full[tt % (2 * C::kStages)], (tt / (2 * C::kStages)) & 1u);
         ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
         const int pos0 = (sg.t0 + gi / C::kPieces) * kKeys + first;     // the piece's first position
         if (ok && pos0 < sg.ctx + a.Ns) {
