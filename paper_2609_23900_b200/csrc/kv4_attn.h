@@ -168,7 +168,7 @@ struct Work : WorkState {
         const int n = b0 + lane < a.B ? w.tiles_of(b0 + lane, &cx, &cr) : 0;
         const int span = n > 0 ? (n + kCost) * upb : 0;
         int upto = span;
-#pragma unroll
+#pragma unroll 1
         for (int d = 1; d < 32; d *= 2) {
           const int x = __shfl_up_sync(0xffffffffu, upto, d);
           if (lane >= d) upto += x;
@@ -234,14 +234,15 @@ struct Work : WorkState {
       g = g_unit + nt + kCost < g_end ? g_unit + nt + kCost : g_end;
       if (lo >= hi) continue;                            // only idle positions of this unit fall into the share
       const int u = b * upb + q;
-      s->b = b; s->hkv = q / a.RT; s->rt = q - s->hkv * a.RT;
+      s->b = b; s->hkv = a.RT == 1 ? q : q / a.RT; s->rt = q - s->hkv * a.RT;
       tiles_of(b, &s->ctx, &s->crow);
       s->t0 = lo - first;
       s->n = hi - lo;
       s->slot = u + blockIdx.x;
       s->unit = u;
-      s->slot0 = u + first / per;
-      s->nslots = (first + nt - 1) / per - first / per + 1;
+      const int c0 = first / per;
+      s->slot0 = u + c0;
+      s->nslots = (first + nt - 1) / per - c0 + 1;
       return true;
     }
     return false;

@@ -567,11 +567,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           tmem_ld32(tmem_lane + kColO + half * 64 + c, orr);
           tmem_ld_wait();
           if (!row_ok) continue;
+          const uint32_t nan = nan_cols >> (half * 4 + (c >> 4));
+          const float f[2] = {nan & 1u ? __uint_as_float(0x7FC00000u) : inv, nan & 2u ? __uint_as_float(0x7FC00000u) : inv};
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const bool nan = (nan_cols >> (half * 4 + (c + e) / 16)) & 1u;
-            orr[e] = bad ? 0u : nan ? 0x7FC00000u : __float_as_uint(__uint_as_float(orr[e]) * inv);
-          }
+          for (int e = 0; e < 32; ++e) orr[e] = bad ? 0u : __float_as_uint(__uint_as_float(orr[e]) * f[e >> 4]);
           if (whole && a.out_bf16) {
             uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * kDh + half * 64 + c);
 #pragma unroll
