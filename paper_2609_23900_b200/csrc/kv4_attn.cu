@@ -55,7 +55,9 @@ template <int NT> struct Small {
     uint32_t bad_page[16];                               // by segment number mod 16: the loader is never that far ahead
   };
   static constexpr int kBytes = kOffCtl + (int)sizeof(Ctl);
-  using W = Work<5, 2, 3>;
+  // A segment costs about as much as eight tiles (sixteen tokens at 16k: 55.2 us, charged five: 59); shares below two tiles, and whole
+  // units up to three tiles longer than a share, save slots.
+  using W = Work<8, 2, 3>;
 };
 static_assert(Small<1>::kBytes <= 227 * 1024 && Small<2>::kBytes <= 227 * 1024, "one CTA per SM");
 

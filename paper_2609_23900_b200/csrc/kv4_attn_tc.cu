@@ -64,7 +64,8 @@ struct Ctl {
 };
 constexpr int kSmemBytes = kOffCtl + (int)sizeof(Ctl);
 static_assert(kSmemBytes + 1024 <= 227 * 1024, "one CTA per SM");
-using TcWork = Work<5, 4, 4>;
+// A segment's start and end cost about as much as eight tiles (8 x 28 nodes at 16k: 67.6 to 70 us, charged five: 71, three: 73 to 75).
+using TcWork = Work<8, 4, 4>;
 
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
