@@ -23,9 +23,9 @@ namespace lumo {
 namespace {
 
 // ---- register form -----------------------------------------------------------------------
-// For up to 8 NT query rows per unit (a token or a short tree of one request times its head group).  Bound by the cache's bytes, so the point is
-// to keep them coming and to spend few instructions on each: one warp issues the bulk copies into a ring of eight tiles, and the others turn
-// codes into matrix operands in registers, without a second trip through shared memory.  A warp takes 16 keys of a tile:
+// For up to 8 NT query rows per unit (a token or a short tree of one request times its head group): one warp issues the bulk copies into a ring
+// of eight tiles, and the others turn codes into matrix operands in registers, without a second trip through shared memory.  A warp takes 16
+// or 32 keys of a tile at a time (NT = 1: 32, two chains of products to overlap), sixteen of them thus:
 //
 //   S^T [16 keys x 8 rows] = K Q^T, eight m16n8k16 products; lane (g, t) of a warp (g = lane / 4, t = lane % 4) supplies elements
 //       [32 t, 32 t + 32) of two keys, one 16-byte read each: which element stands at which place of the inner dimension is free as long as
@@ -35,7 +35,10 @@ namespace {
 //       P^T comes out of S^T's accumulators by an 8 x 8 transposition across the warp.
 //
 // Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
-// The instruction count (about 420 per 16 keys and warp, of which 320 turn codes into f16) is near the time the bytes take.
+// A tile takes each scheduler 720 instructions (90 for 16 keys and scheduler; three quarters turn codes into f16), and the SM's share of the
+// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 55 to 57 us, 4.1 TB/s;
+// one token at 4k: 12.2 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
+// merge the rest.
 template <int NT> struct Small {
   static constexpr int kWarps = NT == 1 ? 15 : 11;       // consumers; with the loader a multiple of four: 128 registers a thread, 168 for NT = 2
   static constexpr int kSub = NT == 1 ? 2 : 1;           // groups of sixteen keys a warp takes at a time
@@ -532,7 +535,10 @@ cudaError_t launch_small(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   return launch_kernel(kv4_attn_small_kernel<NT>, dim3(plan.a.C), dim3(Small<NT>::kThreads), Small<NT>::kBytes, st, pdl, plan.a);
 }
 
-// rows of a row tile: the register form up to sixteen, the tensor-memory form (kv4_attn_tc.cu) beyond
+// Rows of a row tile: the register form up to sixteen, the tensor-memory form (kv4_attn_tc.cu) beyond.  The latter's 128-row tile costs the same
+// however many rows are in use; the register form's work grows with them.  Register form against tensor memory, us: 16 sequences at 16k
+// with 4, 8 and 16 rows 57.6, 61.8, 95.2 against 109; 4 at 8k with 20 and 32 rows (in tiles of sixteen) 33.9, 37.5 against 25.6, 26.5; 8
+// at 16k with 32 rows 95.3 against 61.4.
 int rows_per_tile(int G, int N) { return G * N <= 8 ? 8 : G * N <= 16 ? 16 : 128; }
 
 }  // namespace

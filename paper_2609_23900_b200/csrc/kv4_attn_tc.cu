@@ -17,10 +17,13 @@
 //                are two, each with one commit and a wait or two a tile, and one issues while the other waits.  Q lies in shared memory: the
 //                tensor core reads it from there at the same rate (1024 cycles for both products either way, measured)
 //
-// What bounds it: shared memory carries 164 KB a tile (codes written and read, operands written and read by the tensor core), 1312 cycles at
-// 128 bytes a cycle; the two products take 1024 cycles, the exponentials 1024 on their own units, and the instructions of the softmax and
-// of the conversion about 1000 of the four schedulers.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the
-// memory.
+// What bounds it: a tile takes an SM 1850 cycles once all warps are at work (8 x 28 nodes at 16k; counters by the profiler).  In them the two
+// products take 1024, the exponentials 1024 on their units, the arithmetic units 1010 (half of it codes to f16 and back to pairs), and
+// each scheduler issues 1390 instructions: no unit is full, but five warps a scheduler find something to issue in three cycles of four at
+// best.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the memory.  Around the tiles a CTA spends 10 thousand cycles
+// until its first logits (lengths, page numbers, first copies and first instructions, one after another) and 4 to 6 thousand on the
+// read-out.  Measured, with the merge: 4 x 8 nodes at 8k 26.5 us, 8 x 28 at 16k 69 us (680 TFLOP/s), 64 nodes at 128k 161 us (850 TFLOP/s, at
+// 1.64 GHz under the power limit).
 #include "f32x2.h"
 #include "kv4_attn.h"
 
@@ -137,13 +140,13 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 __device__ __forceinline__ void pair_sync(int bar) { asm volatile("barrier.cta.sync %0, 64;\n" ::"r"(bar) : "memory"); }
-
 __device__ __forceinline__ void pair_arrive(int bar) { asm volatile("barrier.cta.arrive %0, 64;\n" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}// Visibility of 64 consecutive keys from suffix slot s0 on (negative: keys of the committed context, always visible), from a
+}
+// Visibility of 64 consecutive keys from suffix slot s0 on (negative: keys of the committed context, always visible), from a
 // node's 256-bit row over the suffix.
 __device__ __forceinline__ unsigned long long visible64(const uint32_t* row, int s0) {
   if (s0 >= kMaxAttnSlots) return 0ull;
