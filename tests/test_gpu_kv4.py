@@ -416,6 +416,33 @@ def test_captured_replayed_and_on_another_stream(N):
     del g
 
 
+@pytest.mark.parametrize("N", [1, 4, 12, 40])
+def test_two_calls_at_once_and_many_times_over(N):
+    """Two batches on two streams, each with its own workspace, forty times: the same bits as each alone."""
+    cases = [Kv4Case(trees("random", 3, N, 5 + i), ctxs, Hq=8, Hkv=2, page=page, seed=21 + i, out=out)
+             for i, (ctxs, page, out) in enumerate([([5000, 130, 2300], 64, torch.bfloat16), ([0, 3100, 77], 16, torch.float32)])]
+    want, sides, wrong = [], [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for c in cases:
+        c.write()
+        c.attend()
+        torch.cuda.synchronize()
+        c.check("alone")
+        want.append((c.d["out"].clone(), c.d["lse"].clone()))
+        wrong.append(torch.zeros((), dtype=torch.int64, device="cuda"))
+    torch.cuda.synchronize()
+    for _ in range(40):
+        for c, s, w, n in zip(cases, sides, want, wrong):
+            with torch.cuda.stream(s):
+                c.d["out"].zero_()
+                c.d["lse"].zero_()
+                c.attend()
+                n += (c.d["out"] != w[0]).sum() + (c.d["lse"] != w[1]).sum()
+    torch.cuda.synchronize()
+    assert [int(n) for n in wrong] == [0, 0]
+    for c in cases:
+        c.check("afterwards")
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 4 GiB: a page at its end holds what was written there."""
     P, H = 128, 8
