@@ -25,6 +25,14 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kFlight = 4;                     // rows on their way per group of lanes
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
+// a b + c where `on`, else c: one predicated instruction (as a branch it made the lanes of a warp part company in every row)
+__device__ __forceinline__ float2 fma2_if(bool on, float2 a, float2 b, float2 c) {
+  asm("{\n.reg .pred p;\nsetp.ne.u32 p, %3, 0;\n@p fma.rn.f32x2 %0, %1, %2, %0;\n}\n"
+      : "+l"(reinterpret_cast<unsigned long long&>(c))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "r"((uint32_t)on));
+  return c;
+}
+
 // two runs of four elements
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
@@ -67,7 +75,7 @@ template <> struct Raw8<float> {
 template <typename T> constexpr int kCtas = sizeof(T) == 2 ? 4 : 2;      // per SM (bf16: 34.2 us at 8192 tokens, three: 35.7)
 
 // Warp w of the grid takes token w / chunks and the heads [(w % chunks) * per, + per) of q's and k's heads together.
-template <typename T, int DH>
+template <typename T, int DH, bool kPairs>
 __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs a, int chunks, int per) {
   constexpr int LPR = DH / 8;                 // lanes per row
   constexpr int NG = 32 / LPR;                // rows a warp works on at a time
@@ -76,8 +84,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs
   const int grp = lane / LPR, vi = lane % LPR;
   // This lane's elements: four from p0 on and four from p1 on.  Style "half": four of the first half and the four that they form pairs with;
   // style "pairs", and elements that are not rotated: eight in a row.
-  const bool within = a.style == 1, split = !within && 4 * vi < half;
-  const int p0 = split ? 4 * vi : within ? 8 * vi : a.rot + 8 * vi - 2 * half;
+  const bool split = !kPairs && 4 * vi < half;
+  const int p0 = split ? 4 * vi : 8 * vi;
   const int gap = split ? half : 4;
   const bool turned = p0 < a.rot;
   pdl_wait();                                 // everything below may belong to earlier kernels
@@ -114,11 +122,14 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs
     const T* src = reinterpret_cast<const T*>(kind ? a.k : a.q) + tok * in_st + p0;
     T* dst = reinterpret_cast<T*>(kind ? a.k_out : a.q_out) + tok * out_st + p0;
     Raw8<T> raw[kFlight];
-    int h = lo + grp - H0;
-    const int n = hi - H0;
+    int left = hi - lo - grp;                 // rows from this group's next one on
+    src += (lo - H0 + grp) * DH;
+    dst += (lo - H0 + grp) * DH;
+    const T* src1 = src + gap;
+    T* dst1 = dst + gap;
 #pragma unroll
     for (int f = 0; f < kFlight; ++f)
-      if (h + f * NG < n) raw[f].load(src + (h + f * NG) * DH, src + (h + f * NG) * DH + gap);
+      if (f * NG < left) raw[f].load(src + f * NG * DH, src1 + f * NG * DH);
     // y_i = inv (A_i x_i + B_i x_partner): weights, cosines and signed sines in one factor each
     float2 A[4], B[4];
     {
@@ -135,9 +146,9 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs
         for (int i = 0; i < 4; ++i) w[i] = add2(w[i], off);
       }
       if (turned) {
-        const int j0 = within ? p0 >> 1 : p0;
+        const int j0 = kPairs ? p0 >> 1 : p0;
         const float4 cv = *reinterpret_cast<const float4*>(&cs[warp][0][j0]), sv = *reinterpret_cast<const float4*>(&cs[warp][1][j0]);
-        if (within) {
+        if (kPairs) {
           c[0] = make_float2(cv.x, cv.x); c[1] = make_float2(cv.y, cv.y); c[2] = make_float2(cv.z, cv.z); c[3] = make_float2(cv.w, cv.w);
           sn[0] = make_float2(-sv.x, sv.x); sn[1] = make_float2(-sv.y, sv.y); sn[2] = make_float2(-sv.z, sv.z); sn[3] = make_float2(-sv.w, sv.w);
         } else {
@@ -149,17 +160,16 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         A[i] = mul2(w[i], c[i]);
-        B[i] = mul2(within ? make_float2(w[i].y, w[i].x) : w[i ^ 2], sn[i]);
+        B[i] = mul2(kPairs ? make_float2(w[i].y, w[i].x) : w[i ^ 2], sn[i]);
       }
     }
     // whole warps go through this: a group beyond its heads works on what it has and stores nothing
-    for (; h - grp < n; h += kFlight * NG) {
+    for (; left + grp > 0; left -= kFlight * NG, src += kFlight * NG * DH, src1 += kFlight * NG * DH, dst += kFlight * NG * DH, dst1 += kFlight * NG * DH) {
 #pragma unroll
       for (int f = 0; f < kFlight; ++f) {
-        const int hh = h + f * NG;
         float2 x[4], y[4];
         raw[f].get(x);
-        if (hh + kFlight * NG < n) raw[f].load(src + (hh + kFlight * NG) * DH, src + (hh + kFlight * NG) * DH + gap);
+        if ((kFlight + f) * NG < left) raw[f].load(src + (kFlight + f) * NG * DH, src1 + (kFlight + f) * NG * DH);
         float inv = 1.f;
         if (a.norm) {
           float2 sq = mul2(x[0], x[0]);
@@ -173,12 +183,12 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) rope_kernel(const RopeArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           y[i] = mul2(A[i], x[i]);
-          if (turned) y[i] = fma2(B[i], within ? make_float2(x[i].y, x[i].x) : x[i ^ 2], y[i]);      // (not with factors of zero: x may be infinite)
+          y[i] = fma2_if(turned, B[i], kPairs ? make_float2(x[i].y, x[i].x) : x[i ^ 2], y[i]);      // (not with factors of zero: x may be infinite)
         }
         const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], inv2);
-        if (hh < n) Raw8<T>::store(dst + hh * DH, dst + hh * DH + gap, y);
+        if (f * NG < left) Raw8<T>::store(dst + f * NG * DH, dst1 + f * NG * DH, y);
       }
     }
   }
@@ -196,7 +206,9 @@ cudaError_t launch_t(const RopeArgs& a, int sms, bool pdl, cudaStream_t st) {
   per = (per + NG - 1) / NG * NG;
   const int chunks = (H + per - 1) / per;
   const long long warps = (long long)a.T * chunks;
-  return launch_kernel(rope_kernel<T, DH>, dim3((unsigned)((warps + kWarps - 1) / kWarps)), dim3(kThreads), 0, st, pdl, a, chunks, per);
+  const dim3 grid((unsigned)((warps + kWarps - 1) / kWarps));
+  if (a.style == 1) return launch_kernel(rope_kernel<T, DH, true>, grid, dim3(kThreads), 0, st, pdl, a, chunks, per);
+  return launch_kernel(rope_kernel<T, DH, false>, grid, dim3(kThreads), 0, st, pdl, a, chunks, per);
 }
 
 template <typename T>
