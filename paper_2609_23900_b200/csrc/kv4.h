@@ -31,10 +31,13 @@ __device__ __forceinline__ float reciprocal(float x) {   // to about an ulp
   asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
   return r;
 }
-// two e2m1 codes (the first in the low half of the byte): nearest, ties to the even code, at most 6
-__device__ __forceinline__ uint32_t e2m1x2_of(float lo, float hi) {
+// eight e2m1 codes (the first in the lowest four bits): nearest, ties to the even code, at most 6
+__device__ __forceinline__ uint32_t e2m1x8_of(const float2* x) {
   uint32_t r;
-  asm("{\n.reg .b8 t;\ncvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\nmov.b32 %0, {t, 0, 0, 0};\n}\n" : "=r"(r) : "f"(lo), "f"(hi));
+  asm("{\n.reg .b8 a, b, c, d;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\ncvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\ncvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\nmov.b32 %0, {a, b, c, d};\n}\n"
+      : "=r"(r) : "f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y), "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y));
   return r;
 }
 // eight codes -> four f16 pairs, exact

@@ -10,7 +10,8 @@
 // does, and no division is needed.
 // Likewise c * s has at most six significant bits: reading back in bf16 is exact.
 //
-// All of it is data movement: sixteen lanes a row of 128 numbers, 16 bytes of bf16 a lane.
+// Sixteen lanes a row of 128 numbers, 16 bytes of bf16 a lane.  At a prompt's size the instructions bound it, not the bytes: some 110 for two
+// rows to quantise and store, 70 to read back (8191 tokens of 8 heads, both ways: 23.6 us, 3.6 TB/s); a tree's entries take a launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -44,14 +45,14 @@ __device__ __forceinline__ uint32_t quantise8(uint4 raw, float down, uint32_t* s
   const float s = e4m3_value(sb);
   const float r = nan || s == 0.f ? 0.f : down * reciprocal(s);
   const float2 r2 = make_float2(r, r);
-  uint32_t codes = 0;
+  float2 q[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     // to f16's 11 bits first; a value of a block without scale becomes a zero of its sign
     const float2 x = mul2(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), r2);
-    const __half2 q = __floats2half2_rn(x.x, x.y);
-    codes |= e2m1x2_of(__low2float(q), __high2float(q)) << (8 * i);
+    q[i] = __half22float2(__floats2half2_rn(x.x, x.y));
   }
+  const uint32_t codes = e2m1x8_of(q);
   return nan ? 0u : codes;
 }
 
@@ -100,8 +101,18 @@ __global__ void __launch_bounds__(kThreads) kv4_write_kernel(const KL L, const K
 
 // Where the listed tokens of a CTA lie: offset of the page's first block, position in the page, whether there is such a place.
 constexpr int kMostTokens = 32;
-struct Places { long long page[kMostTokens]; int at[kMostTokens]; bool ok[kMostTokens]; };
-__device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& t, int t0, int n, bool writes, bool report, Places& p) {
+struct __align__(16) Place { long long page; int at; int ok; };
+// How the sixteen-lane groups of a CTA go through n tokens of `rows` rows: a group keeps its row (of every pass of sixteen) and takes every
+// `side`-th token, so that addresses run on by a constant; with fewer than sixteen rows, groups beyond the last whole token rest.
+struct Walk {
+  int side, token, row;      // tokens side by side; this group's first token; its row in the first pass
+  __device__ __forceinline__ Walk(int grp, int rows) {
+    side = rows >= kGroups ? 1 : kGroups / rows;
+    token = rows >= kGroups ? 0 : grp / rows;
+    row = grp - token * rows;
+  }
+};
+__device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& t, int t0, int n, bool writes, bool report, Place* p) {
   const int i = threadIdx.x;
   if (i >= n) return;
   const int tok = t0 + i;
@@ -109,9 +120,7 @@ __device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& 
   int pg;
   const int st = kv4_token_check(s, row, pos, writes, &pg);
   if (report && t.status) t.status[tok] = st;
-  p.ok[i] = st == LUMO_SEQ_OK && pg >= 0;
-  p.page[i] = (long long)kv4_block(s.Hkv, s.page, pg < 0 ? 0 : pg, 0, 0);
-  p.at[i] = pos & (s.page - 1);
+  p[i] = {(long long)kv4_block(s.Hkv, s.page, pg < 0 ? 0 : pg, 0, 0), pos & (s.page - 1), st == LUMO_SEQ_OK && pg >= 0};
 }
 
 // Tokens listed one by one: entry of token t goes to position pos[t] of row row[t]; row -1 is passed over.  A CTA takes `per` tokens: their
@@ -119,44 +128,41 @@ __device__ __forceinline__ void find_places(const Kv4Shape& s, const Kv4Tokens& 
 template <class KL>
 __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const Kv4Shape s, const Kv4Tokens t, int per) {
   constexpr int kFlight = 4;
-  __shared__ Places places;
+  __shared__ Place places[kMostTokens];
   const int l = blockIdx.y, t0 = blockIdx.x * per, n = min(per, t.T - t0);
   const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
-  const int rows = 2 * s.Hkv, items = n * rows;
-  const float down_k = exp2i(-s.k_exp), down_v = exp2i(-s.v_exp);
-  uint4 raw[kFlight];
-  int where[kFlight];                            // token of the CTA << 16 | row (a head's keys, or Hkv + a head's values); -1: none
-  int tl = grp / rows, r = grp - tl * rows;      // the next one
-  const int step_t = kGroups / rows, step_r = kGroups - step_t * rows;
-  auto fetch = [&]() {
+  const int rows = 2 * s.Hkv;
+  const Walk walk(grp, rows);
+  bool known = false;
+  for (int r0 = 0; r0 < rows; r0 += kGroups) {   // (uniform over the CTA, like the loop below: the shuffles see whole warps)
+    const int r = r0 + walk.row, which = r >= s.Hkv, h = which ? r - s.Hkv : r;      // keys of all heads, then values
+    const bool mine = r < rows && walk.token < walk.side;
+    const float down = exp2i(which ? -s.v_exp : -s.k_exp);
+    const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(which ? L.vn[l] : L.kn[l]) + (t0 + walk.token) * s.kv_stride + h * 128 + lane16 * 8;
+    unsigned char* blk = reinterpret_cast<unsigned char*>(L.pages[l]) + (2 * h + which) * (s.page * kKv4Entry);
+    const long long step = walk.side * s.kv_stride;
+    for (int k0 = 0; k0 < n; k0 += kFlight * walk.side, src += kFlight * step) {
+      uint4 raw[kFlight];
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      raw[f] = make_uint4(0, 0, 0, 0);
-      where[f] = tl < n ? tl << 16 | r : -1;
-      if (tl < n) {
-        const int which = r >= s.Hkv;
-        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(which ? L.vn[l] : L.kn[l]) + (long long)(t0 + tl) * s.kv_stride + (which ? r - s.Hkv : r) * 128;
-        raw[f] = __ldg(reinterpret_cast<const uint4*>(src) + lane16);
+      for (int f = 0; f < kFlight; ++f) {
+        raw[f] = make_uint4(0, 0, 0, 0);
+        if (mine && k0 + f * walk.side + walk.token < n) raw[f] = __ldg(reinterpret_cast<const uint4*>(src + f * step));
       }
-      tl += step_t;
-      r += step_r;
-      if (r >= rows) { r -= rows; ++tl; }
-    }
-  };
-  fetch();
-  find_places(s, t, t0, n, true, l == 0, places);
-  __syncthreads();
-  // uniform over the CTA: the shuffles see whole warps
-  for (int base = 0; base < items; base += kFlight * kGroups) {
-    if (base) fetch();
+      if (!known) {                              // the places are looked up while the first rows are on their way
+        find_places(s, t, t0, n, true, l == 0, places);
+        __syncthreads();
+        known = true;
+      }
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      const int tok = where[f] < 0 ? 0 : where[f] >> 16, rr = where[f] & 0xFFFF, which = rr >= s.Hkv;
-      const int at = places.at[tok];
-      unsigned char* blk = reinterpret_cast<unsigned char*>(L.pages[l]) + places.page[tok] + (which ? 2 * (rr - s.Hkv) + 1 : 2 * rr) * (s.page * kKv4Entry);
-      store_row(blk + at * 64, blk + s.page * 64 + at * 8, raw[f], which ? down_v : down_k, lane16, where[f] >= 0 && places.ok[tok]);
+      for (int f = 0; f < kFlight; ++f) {
+        const int k = k0 + f * walk.side + walk.token;
+        const bool in = mine && k < n;
+        const Place pl = places[in ? k : 0];
+        unsigned char* page = blk + pl.page;
+        store_row(page + pl.at * 64, page + s.page * 64 + pl.at * 8, raw[f], down, lane16, in && pl.ok);
+      }
     }
   }
 }
@@ -165,49 +171,49 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const KL L, const 
 __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const unsigned char* pages, const Kv4Shape s, const Kv4Tokens t, __nv_bfloat16* k_out,
                                                             __nv_bfloat16* v_out, int per) {
   constexpr int kFlight = 8;
-  __shared__ Places places;
+  __shared__ Place places[kMostTokens];
   const int t0 = blockIdx.x * per, n = min(per, t.T - t0);
   const int lane16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
   pdl_wait();          // everything below may belong to earlier kernels
   pdl_trigger();
   const int rows = 2 * s.Hkv;
-  const float up_k = exp2i(s.k_exp), up_v = exp2i(s.v_exp);
+  const Walk walk(grp, rows);
   find_places(s, t, t0, n, false, true, places);
   __syncthreads();
-  int tl = grp / rows, r = grp - tl * rows;
-  const int step_t = kGroups / rows, step_r = kGroups - step_t * rows;
-  while (tl < n) {
-    uint32_t codes[kFlight], sb[kFlight];
-    int where[kFlight];
+  if (walk.token >= walk.side) return;
+  for (int r = walk.row; r < rows; r += kGroups) {
+    const int which = r >= s.Hkv, h = which ? r - s.Hkv : r;
+    const float up = exp2i(which ? s.v_exp : s.k_exp);
+    const unsigned char* blk = pages + (2 * h + which) * (s.page * kKv4Entry);
+    uint4* dst = reinterpret_cast<uint4*>((which ? v_out : k_out) + ((long long)(t0 + walk.token) * s.Hkv + h) * 128) + lane16;
+    const int step = walk.side * s.Hkv * 16;
+    for (int k0 = walk.token; k0 < n; k0 += kFlight * walk.side, dst += kFlight * (long long)step) {
+      uint32_t codes[kFlight], sb[kFlight];
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      codes[f] = 0; sb[f] = 0;
-      where[f] = tl < n ? tl << 16 | r : -1;
-      if (tl < n && places.ok[tl]) {
-        const unsigned char* blk = pages + places.page[tl] + (r >= s.Hkv ? 2 * (r - s.Hkv) + 1 : 2 * r) * (s.page * kKv4Entry);
-        const int at = places.at[tl];
-        codes[f] = reinterpret_cast<const uint32_t*>(blk + at * 64)[lane16];
-        sb[f] = blk[s.page * 64 + at * 8 + (lane16 >> 1)];
+      for (int f = 0; f < kFlight; ++f) {
+        const int k = k0 + f * walk.side;
+        const Place pl = places[k < n ? k : 0];
+        codes[f] = 0; sb[f] = 0;
+        if (k < n && pl.ok) {
+          const unsigned char* page = blk + pl.page;
+          codes[f] = reinterpret_cast<const uint32_t*>(page + pl.at * 64)[lane16];
+          sb[f] = page[s.page * 64 + pl.at * 8 + (lane16 >> 1)];
+        }
       }
-      tl += step_t;
-      r += step_r;
-      if (r >= rows) { r -= rows; ++tl; }
-    }
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      if (where[f] < 0) continue;
-      const int rr = where[f] & 0xFFFF, which = rr >= s.Hkv;
-      const float sc = e4m3_value(sb[f]) * (which ? up_v : up_k);
-      uint32_t h2[4], w[4];
-      e2m1x8_to_half2(codes[f], h2);
+      for (int f = 0; f < kFlight; ++f) {
+        if (k0 + f * walk.side >= n) continue;
+        const float sc = e4m3_value(sb[f]) * up;
+        uint32_t h2[4], w[4];
+        e2m1x8_to_half2(codes[f], h2);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 v = mul2(__half22float2(*reinterpret_cast<const __half2*>(&h2[k])), make_float2(sc, sc));
-        const __nv_bfloat162 o = __floats2bfloat162_rn(v.x, v.y);
-        w[k] = *reinterpret_cast<const uint32_t*>(&o);
+        for (int k = 0; k < 4; ++k) {
+          const float2 v = mul2(__half22float2(*reinterpret_cast<const __half2*>(&h2[k])), make_float2(sc, sc));
+          const __nv_bfloat162 o = __floats2bfloat162_rn(v.x, v.y);
+          w[k] = *reinterpret_cast<const uint32_t*>(&o);
+        }
+        dst[(long long)f * step] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      __nv_bfloat16* dst = (which ? v_out : k_out) + ((long long)(t0 + (where[f] >> 16)) * s.Hkv + (which ? rr - s.Hkv : rr)) * 128;
-      reinterpret_cast<uint4*>(dst)[lane16] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -271,7 +277,7 @@ cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers
   return launch_kernel(kv4_write_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s);
 }
 
-// Tokens a CTA takes: 128 rows' worth (8191 tokens of 8 KV heads appended and read back: 26.5 us; 64 rows: 30.2, 256: 31.9), fewer while the
+// Tokens a CTA takes: 128 rows' worth (8191 tokens of 8 KV heads appended and read back: 23.6 us; 64 rows: 27.6, 192: 24.9), fewer while the
 // GPU is not covered.
 static int tokens_per_cta(int T, int Hkv, int sms) {
   int per = 128 / (2 * Hkv);
