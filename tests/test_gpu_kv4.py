@@ -101,6 +101,42 @@ def test_append_and_read_are_the_oracles_bit_for_bit(page, e):
                 assert np.array_equal(back[t, h].double().cpu().numpy(), ref, equal_nan=True), (t, h, w)
 
 
+@pytest.mark.parametrize("H", [1, 2, 5, 8, 10, 33])
+def test_long_lists_of_any_number_of_heads(H):
+    """Several tokens a CTA, heads that do not fill its groups of lanes or take several passes: what is read back is what was quantised."""
+    rs = np.random.default_rng(H)
+    T, page = 1501, 32
+    per = -(-T // page)
+    table = torch.from_numpy(rs.permutation(per + 3)[None, :per].astype(np.int32)).cuda()
+    pages = torch.from_numpy(rs.integers(0, 256, (per + 3, H, 2, page * 72), dtype=np.uint8)).cuda()
+    before = pages.clone()
+    k, v = (bf16(rs.standard_normal((T, H, 128))) for _ in range(2))
+    layer = binding.Kv4Layer(Hq=H, Hkv=H, pages=pages, table=table, page_size=page, k_new=k, v_new=v)
+    pos = torch.from_numpy(rs.permutation(T).astype(np.int32)).cuda()
+    row = torch.zeros_like(pos)
+    row[7] = -1                                                            # passed over
+    status = torch.full((T + 5,), -1, dtype=torch.int32, device="cuda")
+    ctx().kv4_append([layer], row, pos, status=status)
+    kb, vb = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    ctx().kv4_read(layer, row, pos, kb, vb)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] * T + [-1] * 5
+    for x, back in ((k, kb), (v, vb)):
+        pick = np.unique(np.concatenate([[0, 7, T - 1], rs.choice(T, max(8, 300 // H), replace=False)]))
+        want = torch.from_numpy(O.quantise(x[pick].double().cpu().numpy()))
+        want[list(pick).index(7)] = 0
+        assert torch.equal(back[pick].double().cpu(), want)
+        assert bool((back[7] == 0).all()) and not bool((back == 7.0).all(-1).any())
+    hole = int(pos[7])                                                     # its entry, the last page's rest and the spare pages are as they were
+    pg, at = int(table[0, hole // page]), hole % page
+    assert torch.equal(pages[pg, :, :, at * 64:at * 64 + 64], before[pg, :, :, at * 64:at * 64 + 64])
+    spare = sorted(set(range(per + 3)) - set(table[0].tolist()))
+    assert torch.equal(pages[spare], before[spare])
+    last, used = int(table[0, -1]), T % page
+    assert torch.equal(pages[last, :, :, used * 64:page * 64], before[last, :, :, used * 64:page * 64])
+    assert torch.equal(pages[last, :, :, page * 64 + used * 8:], before[last, :, :, page * 64 + used * 8:])
+
+
 def test_every_quotient_lands_on_the_right_side():
     """All bf16 numbers of four binades against a block maximum that runs through all scales of a binade: codes as by exhaustive search."""
     bits = torch.arange(0x3E00, 0x4000, dtype=torch.int32)               # 0.125 to 2, 512 numbers
