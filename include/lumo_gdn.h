@@ -515,7 +515,8 @@ int64_t lumo_kv4_work_bytes(const lumo_ctx* ctx, const lumo_tree_desc* desc, int
 /* lumo_tree_attention over the 4-bit pages.  Codes times scales are exact in f16; probabilities enter the second product rounded to
  * f16; all sums are fp32.  A NaN held in a page reaches the outputs of the nodes that see its position and no others; bytes of
  * positions that nobody sees may be anything.  Bitwise reproducible for a given device, shape and n_splits.  Enqueues only and
- * allocates nothing; partial results live in `work`, which the layers of a call use one after another. */
+ * allocates nothing; partial results live in `work`, which the layers of a call use one after another.  If a bounded device-side wait runs
+ * out, every sequence of the layer gets LUMO_SEQ_TIMEOUT and the layer's outputs are invalid. */
 int lumo_kv4_attention(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, void* stream);
 /* lumo_kv_publish over the 4-bit pages: the accepted entries move as they are, bit for bit. */
 int lumo_kv4_publish(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4_args* layers, int n_layers, const int32_t* accepted_dev,

@@ -3,13 +3,14 @@
 //   y = x * rsqrt(mean(x^2) + eps) * (w + offset);   pairs (a, b) of y's first `rot` elements become
 //   (a cos t - b sin t, a sin t + b cos t) * m,      t = position(axis of the pair) * inv_freq[pair]
 //
-// Each element is read once and written once; what bounds the kernel at a prompt's size is that traffic together with the instructions (about
-// 90 for two rows of 128).  A row (one head of one token) is held by dh / 8 lanes, so that both elements of a pair are in one lane (with the
-// partner fetched by shuffles: 36.2 us instead of 34.2); sums and products are fp32, rounded once at the end.  A warp takes one token and a
-// run of its heads, without a barrier in the CTA: it works out the token's angles, in 64 bits (at position 10^6 an fp32 product is off by
-// 0.03 rad), reduced to a fraction of a turn and handed to sincospif, keeps cosines, sines and weights in registers as one factor an
-// element, and goes through its heads with four rows per group of lanes on their way.
-// Measured: 8192 tokens of 32 + 8 heads of 128 in bf16, 34.2 us, 4.9 TB/s; one token, and 224, 4.6 us (a launch).
+// Each element is read once and written once; what bounds the kernel at a prompt's size is that traffic together with the instructions (97
+// for two rows of 128, angles included).  A row (one head of one token) is held by dh / 8 lanes, so that both elements of a pair are in one
+// lane; sums and products are fp32, rounded once at the end.  A warp takes one token and a run of its heads, without a barrier in the CTA: it
+// works out the token's angles, in 64 bits (at position 10^6 an fp32 product is off by 0.03 rad), reduced to a fraction of a turn and
+// handed to sincospif, keeps cosines, sines and weights in registers as one factor an element, and goes through its heads with four rows
+// per group of lanes on their way.
+// Measured: 8192 tokens of 32 + 8 heads of 128 in bf16, 30.7 us, 5.5 TB/s (with partners fetched by shuffles 36.2, with a branch for elements
+// that are not rotated 34.2); one token, and 224, 4.3 us (a launch).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -72,7 +73,7 @@ template <> struct Raw8<float> {
   }
 };
 
-template <typename T> constexpr int kCtas = sizeof(T) == 2 ? 4 : 2;      // per SM (bf16: 34.2 us at 8192 tokens, three: 35.7)
+template <typename T> constexpr int kCtas = sizeof(T) == 2 ? 4 : 2;      // per SM (bf16: 31.4 us at 8192 tokens, three: 34.4)
 
 // Warp w of the grid takes token w / chunks and the heads [(w % chunks) * per, + per) of q's and k's heads together.
 template <typename T, int DH, bool kPairs>
@@ -199,8 +200,8 @@ cudaError_t launch_t(const RopeArgs& a, int sms, bool pdl, cudaStream_t st) {
   constexpr int NG = 32 * 8 / DH;
   const int H = a.Hq + a.Hkv;
   // Few tokens: as many warps a token as give the GPU sixteen an SM, down to one round of loads each.  Many tokens: a warp goes through all
-  // heads of its token, and its angles are worked out once (two warps a token: 39 us instead of 36 at 8192 tokens of 40 heads; rows dealt
-  // out evenly over a resident grid: no gain either).
+  // heads of its token, and its angles are worked out once (two warps a token: 33.2 us instead of 30.7 at 8192 tokens of 40 heads; rows
+  // dealt out evenly over a resident grid: no gain either).
   const long long rows_per_warp = ((long long)a.T * H + 16LL * sms - 1) / (16LL * sms);
   int per = (int)(rows_per_warp < H ? rows_per_warp : H);
   per = (per + NG - 1) / NG * NG;
