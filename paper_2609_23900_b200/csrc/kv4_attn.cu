@@ -58,9 +58,9 @@ template <int NT> struct Small {
     uint32_t bad_page[16];                               // by segment number mod 16: the loader is never that far ahead
   };
   static constexpr int kBytes = kOffCtl + (int)sizeof(Ctl);
-  // A segment costs about as much as eight tiles (sixteen tokens at 16k: 55.2 us, charged five: 59); shares below two tiles, and whole
-  // units up to three tiles longer than a share, save slots.
-  using W = Work<8, 2, 3>;
+  // A segment costs about as much as twelve tiles (sixteen tokens at 16k, one at 4k: 55.6 and 12.1 us; charged five 59 and 12.7, charged
+  // sixteen 57.8 and 12.4); no share below two tiles (four: 12.7 at 4k), and whole units up to three tiles longer than a share.
+  using W = Work<12, 2, 3>;
 };
 static_assert(Small<1>::kBytes <= 227 * 1024 && Small<2>::kBytes <= 227 * 1024, "one CTA per SM");
 
