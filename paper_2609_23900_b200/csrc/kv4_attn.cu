@@ -36,8 +36,8 @@ namespace {
 //
 // Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
 // A tile takes each scheduler 720 instructions (90 for 16 keys and scheduler; three quarters turn codes into f16), and the SM's share of the
-// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 55 to 57 us, 4.1 TB/s;
-// one token at 4k: 12.2 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
+// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 55.6 us, 4.2 TB/s;
+// one token at 4k: 12.1 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
 // merge the rest.
 template <int NT> struct Small {
   static constexpr int kWarps = NT == 1 ? 15 : 11;       // consumers; with the loader a multiple of four: 128 registers a thread, 168 for NT = 2
