@@ -543,7 +543,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       have = work.next(&sgn);
       if (have && sgn.n > 0) mul_next = store_q(sgn);
       // ... then the last O product, the two groups' sums, normalise and write the slot
-      const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;   // (both loaders see the same pages)
       const bool last = (int)((it - 1) & 1u) == half;    // this group had the last tile: its reference is the accumulator's
       if (last) sm.ref[row] = m;
       pair_sync(pair_bar);
@@ -551,6 +550,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       // would otherwise take for the last one's)
       if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
       tc_fence_after();
+      // (behind the wait: the last tile has been loaded; both loaders see the same pages)
+      const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;
       const float mine = m;
       m = sm.ref[row];
       if (m != mine && mine != -INFINITY) l *= ex2(mine - m);

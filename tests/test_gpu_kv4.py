@@ -348,6 +348,32 @@ def test_bad_sequences_are_left_alone_and_the_others_served():
     assert set(changed) <= set(c.table[c.row[5]].tolist())
 
 
+@pytest.mark.parametrize("N", [1, 4, 12])
+@pytest.mark.parametrize("ctx_len", [100, 200, 330, 700, 1500])
+def test_a_page_missing_at_the_very_end(N, ctx_len):
+    """The last tile's page is the one that is missing, every call in a row: no output and no status goes by what was known before it."""
+    c = Kv4Case(trees("random", 2, N, 3), [ctx_len, ctx_len // 2], Hq=8, Hkv=2, page=16, seed=31, n_splits=1)
+    c.write()
+    last = (ctx_len + c.Ns - 1) // 16
+    keep = int(c.table[c.row[0], last])
+    table, want = c.d["table"], None
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    c.attend()
+    torch.cuda.synchronize()
+    c.check("whole")
+    want = c.d["out"].clone()
+    for _ in range(30):
+        table[int(c.row[0]), last] = -1
+        c.attend()
+        wrong += (c.d["out"][0] != 0).sum() + (c.d["lse"][0] != 0).sum() + (c.d["out"][1] != want[1]).sum()
+        wrong += (c.d["status"] != torch.tensor([O.SEQ_BAD_PAGE, 0], dtype=torch.int32, device="cuda")).sum()
+        table[int(c.row[0]), last] = keep
+        c.attend()
+        wrong += (c.d["out"] != want).sum() + (c.d["status"] != 0).sum()
+    torch.cuda.synchronize()
+    assert int(wrong) == 0
+
+
 def test_publication_refuses_what_is_no_path():
     c = Kv4Case([[-1, 0, 1, 0]] * 5, [20] * 5, Hq=2, Hkv=1, page=16, seed=4)
     c.write()
