@@ -216,6 +216,8 @@ def _rows_ptr(t: Optional[torch.Tensor], heads: int, dh: int, name: str):
     for i in range(t.dim() - 3):
         if t.shape[i] != 1 and t.stride(i) != stride * int(np.prod(t.shape[i + 1:-2])):
             raise ValueError(f"{name}: the tokens must be evenly spaced")
+    if stride < heads * dh:                                  # 0 of an expanded tensor among them, which the library takes for heads * dh
+        raise ValueError(f"{name}: the tokens must not share elements")
     return t.data_ptr(), stride
 
 

@@ -1,0 +1,67 @@
+"""Which tensors the calls around the paged 4-bit cache take, without a GPU: every word that a call reads or writes is inside the tensors it is
+given, and nothing is refused that could be passed on.  Host tensors that call themselves CUDA tensors go through the binding; a host-only
+context refuses to launch what gets as far as the library."""
+import numpy as np
+import pytest
+import torch
+
+import __graft_entry__ as entry
+
+entry.build()
+
+from paper_2609_23900_b200 import binding as B               # noqa: E402
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = property(lambda self: True)
+
+
+def gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def bf16(*shape):
+    return gpu(torch.zeros(*shape, dtype=torch.bfloat16))
+
+
+def i32(*shape):
+    return gpu(torch.zeros(*shape, dtype=torch.int32))
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return B.Context(-1)
+
+
+def reaches_launch(call):
+    with pytest.raises(B.LumoError, match="host-only"):
+        call()
+
+
+def refused(call, what):
+    with pytest.raises(ValueError, match=what):
+        call()
+
+
+def cache(H=2, page=16):
+    return dict(Hq=H, Hkv=H, pages=gpu(torch.zeros(4, H, 2, page * 72, dtype=torch.uint8)), table=i32(2, 3), page_size=page)
+
+
+# ---- tokens that are one and the same row ----
+@pytest.mark.parametrize("shape,expanded", [((1, 2, 128), (5, 2, 128)), ((1, 1, 2, 128), (3, 4, 2, 128)), ((1, 4, 2, 128), (3, 4, 2, 128)),
+                                            ((3, 1, 2, 128), (3, 4, 2, 128))])
+def test_an_expanded_tensor_is_refused(shape, expanded):
+    """Its tokens are not heads * dh elements apart (the library takes a stride of 0 for that), so T rows would be read where there is one."""
+    x, one = bf16(*expanded), bf16(*shape).expand(*expanded)
+    assert isinstance(one, OnGpu) and 0 in one.stride()
+    for kw in (dict(q=one, q_out=x), dict(q=x, q_out=one), dict(q=x, q_out=x, k=one, k_out=x), dict(q=x, q_out=x, k=x, k_out=one)):
+        refused(lambda: B.QkNormRope(**kw), "tokens")
+    for kw in (dict(q=one), dict(k_new=one, v_new=one), dict(k_new=one, v_new=x), dict(k_new=x, v_new=one)):
+        refused(lambda: B.Kv4Layer(**cache(), **kw), "tokens")
+
+
+def test_overlapping_tokens_are_refused():
+    part = gpu(torch.zeros(4096, dtype=torch.bfloat16)).as_strided((5, 2, 128), (128, 128, 1))
+    refused(lambda: B.QkNormRope(q=part, q_out=bf16(5, 2, 128)), "tokens")
+    refused(lambda: B.Kv4Layer(**cache(), k_new=part, v_new=part), "tokens")
+    assert B._rows_ptr(bf16(1, 2, 128).expand(1, 2, 128), 2, 128, "q")[1] == 0          # one token: nothing to be apart
