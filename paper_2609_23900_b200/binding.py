@@ -212,10 +212,12 @@ def _rows_ptr(t: Optional[torch.Tensor], heads: int, dh: int, name: str):
         raise ValueError(f"{name} must be a CUDA tensor [..., {heads}, {dh}] with adjacent heads")
     if t.is_contiguous():
         return t.data_ptr(), 0
-    stride = t.stride(-3)
-    for i in range(t.dim() - 3):
-        if t.shape[i] != 1 and t.stride(i) != stride * int(np.prod(t.shape[i + 1:-2])):
+    axes = [(n, st) for n, st in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]      # (an axis of one entry has no say in the spacing)
+    stride, tokens = axes[-1][1], 1
+    for n, st in reversed(axes):
+        if st != stride * tokens:
             raise ValueError(f"{name}: the tokens must be evenly spaced")
+        tokens *= n
     if stride < heads * dh:                                  # 0 of an expanded tensor among them, which the library takes for heads * dh
         raise ValueError(f"{name}: the tokens must not share elements")
     return t.data_ptr(), stride

@@ -65,3 +65,28 @@ def test_overlapping_tokens_are_refused():
     refused(lambda: B.QkNormRope(q=part, q_out=bf16(5, 2, 128)), "tokens")
     refused(lambda: B.Kv4Layer(**cache(), k_new=part, v_new=part), "tokens")
     assert B._rows_ptr(bf16(1, 2, 128).expand(1, 2, 128), 2, 128, "q")[1] == 0          # one token: nothing to be apart
+
+
+# ---- axes of one entry ----
+def test_an_axis_of_one_entry_has_no_say_in_the_spacing():
+    """Parts of a packed projection of one token a sequence: the stride of the axis of size one says nothing."""
+    packed = bf16(3, 6144)                                   # 32 + 8 + 8 heads
+    q, k, v = packed[:, :4096].view(3, 1, 32, 128), packed[:, 4096:5120].view(3, 1, 8, 128), packed[:, 5120:].view(3, 1, 8, 128)
+    one = packed[:, None].unflatten(-1, (48, 128))[:, :, :32]
+    for t, heads in ((q, 32), (k, 8), (v, 8), (one, 32), (packed[:, :4096].view(3, 1, 1, 32, 128), 32), (packed[:, :4096].view(1, 3, 1, 32, 128), 32)):
+        assert B._rows_ptr(t, heads, 128, "t") == (t.data_ptr(), 6144)
+    assert B._rows_ptr(packed[:1, :4096].view(1, 1, 32, 128), 32, 128, "t")[1] == 0           # one token
+    a = B.Kv4Layer(**cache(8), q=None, k_new=k, v_new=v).args
+    assert a.kv_stride == 6144
+    a = B.QkNormRope(q=q, k=k, q_out=q, k_out=bf16(3, 1, 8, 128)).args
+    assert (a.T, a.q_stride, a.k_stride, a.q_out_stride, a.k_out_stride) == (3, 6144, 6144, 6144, 0)
+    deep = bf16(2, 5, 6144)[..., :4096].unflatten(-1, (32, 128))
+    assert B._rows_ptr(deep, 32, 128, "t")[1] == 6144 and B._rows_ptr(deep[:, None], 32, 128, "t")[1] == 6144
+
+
+def test_unevenly_spaced_tokens_are_refused():
+    x = bf16(2, 5, 6144)[..., :4096].unflatten(-1, (32, 128))
+    for t in (x[:, :4], x[:, ::2], x.transpose(0, 1)):
+        refused(lambda: B._rows_ptr(t, 32, 128, "t"), "evenly spaced")
+    assert B._rows_ptr(x[:, 1:2], 32, 128, "t")[1] == 5 * 6144
+    assert B._rows_ptr(x[1:], 32, 128, "t")[1] == 6144
