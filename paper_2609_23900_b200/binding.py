@@ -238,6 +238,9 @@ def _listed(first: torch.Tensor, **tensors) -> int:
     return n
 
 
+_ANY = 1 << 62           # room of a tensor that is not given: the library says which ones a call needs
+
+
 def pages_work_ints(n_rows: int, n_pages: int) -> int:
     """Ints of scratch a page table's calls need."""
     return int(_lib.lumo_pages_work_ints(int(n_rows), int(n_pages)))
@@ -402,20 +405,34 @@ class Context:
 
     @staticmethod
     def pack_kv4(layers: Sequence["Kv4Layer"]):
-        return (_Kv4Args * len(layers))(*[l.args for l in layers])
+        """ctypes array of the layers' argument blocks (reusable across calls); keeps the layers, and knows how much their tensors hold."""
+        arr = (_Kv4Args * len(layers))(*[l.args for l in layers])
+        arr.layers = list(layers)
+        arr.new_tokens = min((l.new_tokens for l in layers), default=_ANY)
+        return arr
+
+    @staticmethod
+    def _kv4(layers):
+        if not isinstance(layers, ctypes.Array):
+            return Context.pack_kv4(layers)
+        if not hasattr(layers, "layers"):
+            raise ValueError("an array of layers has to come from pack_kv4")
+        return layers
 
     def kv4_work_bytes(self, desc: "TreeDesc", Hq: int, Hkv: int, n_splits: int = 0) -> int:
         """Bytes of workspace ``kv4_attention`` needs (Kv4Layer's ``work``)."""
         return int(_lib.lumo_kv4_work_bytes(self._h, desc._h, int(Hq), int(Hkv), int(n_splits)))
 
     def kv4_write_tree(self, desc: "TreeDesc", layers, stream=None):
-        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        arr = self._kv4(layers)
         self._check(_lib.lumo_kv4_write_tree(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
         """Entries of listed tokens (int32 rows and positions, [T]); ``status``, if given, gets a word per token."""
-        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        arr = self._kv4(layers)
         T = _listed(tok_row, tok_row=tok_row, tok_pos=tok_pos, status=status)
+        if T > arr.new_tokens:
+            raise ValueError(f"k_new and v_new hold {arr.new_tokens} tokens, {T} are listed")
         self._check(_lib.lumo_kv4_append(self._h, arr, len(arr), T, _ptr(tok_row), _ptr(tok_pos), _ptr(status), _stream(stream)))
 
     def kv4_read(self, layer: "Kv4Layer", tok_row: torch.Tensor, tok_pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
@@ -429,12 +446,12 @@ class Context:
                                        _stream(stream)))
 
     def kv4_attention(self, desc: "TreeDesc", layers, stream=None):
-        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        arr = self._kv4(layers)
         self._check(_lib.lumo_kv4_attention(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_publish(self, desc: "TreeDesc", layers, accepted: torch.Tensor, length: torch.Tensor,
                     ctx_len_out: Optional[torch.Tensor] = None, stream=None):
-        arr = layers if isinstance(layers, ctypes.Array) else self.pack_kv4(layers)
+        arr = self._kv4(layers)
         self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), int(accepted.shape[1]),
                                           _ptr(ctx_len_out), _stream(stream)))
 
@@ -668,6 +685,7 @@ class Kv4Layer:
             setattr(a, name, _ptr(self.tensors[name]))
         a.work_bytes = work.numel() * work.element_size() if work is not None else 0
         self.args = a
+        self.new_tokens = min((t.numel() // (int(Hkv) * 128) for t in (k_new, v_new) if t is not None), default=_ANY)
 
 
 class PageTable:

@@ -28,8 +28,9 @@ def i32(*shape):
     return gpu(torch.zeros(*shape, dtype=torch.int32))
 
 
-@pytest.fixture(scope="module")
-def ctx():
+@pytest.fixture
+def ctx(monkeypatch):
+    monkeypatch.setattr(B, "_stream", lambda stream: None)   # (the current stream is a question to the driver)
     return B.Context(-1)
 
 
@@ -90,3 +91,34 @@ def test_unevenly_spaced_tokens_are_refused():
         refused(lambda: B._rows_ptr(t, 32, 128, "t"), "evenly spaced")
     assert B._rows_ptr(x[:, 1:2], 32, 128, "t")[1] == 5 * 6144
     assert B._rows_ptr(x[1:], 32, 128, "t")[1] == 6144
+
+
+# ---- how many tokens the keys and values hold ----
+def test_a_list_is_no_longer_than_the_keys(ctx):
+    """Also for layers packed beforehand, and by the layer that has the fewest."""
+    seven, five = B.Kv4Layer(**cache(), k_new=bf16(7, 2, 128), v_new=bf16(7, 2, 128)), B.Kv4Layer(**cache(), k_new=bf16(5, 2, 128), v_new=bf16(5, 2, 128))
+    uneven = B.Kv4Layer(**cache(), k_new=bf16(9, 2, 128), v_new=bf16(6, 2, 128))
+    tree = B.Kv4Layer(**cache(), k_new=bf16(2, 3, 2, 128), v_new=bf16(2, 3, 2, 128))
+    assert (seven.new_tokens, uneven.new_tokens, tree.new_tokens) == (7, 6, 6)
+    for layer, n in ((seven, 7), (five, 5), (uneven, 6), (tree, 6)):
+        for layers in ([layer], ctx.pack_kv4([layer])):
+            reaches_launch(lambda: ctx.kv4_append(layers, i32(n), i32(n)))
+            reaches_launch(lambda: ctx.kv4_append(layers, i32(1), i32(1)))
+            refused(lambda: ctx.kv4_append(layers, i32(n + 1), i32(n + 1)), "k_new and v_new")
+    shared = [B.Kv4Layer(**{**cache(), "table": seven.tensors["table"]}, k_new=bf16(n, 2, 128), v_new=bf16(n, 2, 128)) for n in (8, 5, 7)]
+    for layers in (shared, ctx.pack_kv4(shared)):
+        reaches_launch(lambda: ctx.kv4_append(layers, i32(5), i32(5)))
+        refused(lambda: ctx.kv4_append(layers, i32(6), i32(6)), "k_new and v_new")
+    with pytest.raises(B.LumoError, match="k_new"):
+        ctx.kv4_append([B.Kv4Layer(**cache())], i32(1), i32(1))
+
+
+def test_packed_layers_keep_their_tensors(ctx):
+    import weakref
+    keys = bf16(3, 2, 128)
+    gone = weakref.ref(keys)
+    packed = ctx.pack_kv4([B.Kv4Layer(**cache(), k_new=keys, v_new=bf16(3, 2, 128))])
+    del keys
+    assert gone() is not None and len(packed) == 1
+    with pytest.raises(ValueError, match="pack_kv4"):                     # an array of another making says nothing of its tensors
+        ctx.kv4_append((B._Kv4Args * 1)(packed[0]), i32(1), i32(1))
