@@ -408,7 +408,8 @@ class Context:
         """ctypes array of the layers' argument blocks (reusable across calls); keeps the layers, and knows how much their tensors hold."""
         arr = (_Kv4Args * len(layers))(*[l.args for l in layers])
         arr.layers = list(layers)
-        arr.new_tokens = min((l.new_tokens for l in layers), default=_ANY)
+        for name in ("sequences", "nodes", "new_tokens"):
+            setattr(arr, name, min((getattr(l, name) for l in layers), default=_ANY))
         return arr
 
     @staticmethod
@@ -419,12 +420,22 @@ class Context:
             raise ValueError("an array of layers has to come from pack_kv4")
         return layers
 
+    @staticmethod
+    def _kv4_on(desc: "TreeDesc", layers, nodes: Optional[str] = None):
+        """Packed layers whose tensors hold a word for each of desc's sequences and (``nodes``: which ones) a token for each of its nodes."""
+        arr = Context._kv4(layers)
+        if desc.B > arr.sequences:
+            raise ValueError("ctx_len, cache_row or status is too small for these trees")
+        if nodes is not None and desc.B * desc.N > getattr(arr, nodes):
+            raise ValueError(f"{'q, out or lse' if nodes == 'nodes' else 'k_new or v_new'} is too small for these trees")
+        return arr
+
     def kv4_work_bytes(self, desc: "TreeDesc", Hq: int, Hkv: int, n_splits: int = 0) -> int:
         """Bytes of workspace ``kv4_attention`` needs (Kv4Layer's ``work``)."""
         return int(_lib.lumo_kv4_work_bytes(self._h, desc._h, int(Hq), int(Hkv), int(n_splits)))
 
     def kv4_write_tree(self, desc: "TreeDesc", layers, stream=None):
-        arr = self._kv4(layers)
+        arr = self._kv4_on(desc, layers, "new_tokens")
         self._check(_lib.lumo_kv4_write_tree(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
@@ -446,12 +457,12 @@ class Context:
                                        _stream(stream)))
 
     def kv4_attention(self, desc: "TreeDesc", layers, stream=None):
-        arr = self._kv4(layers)
+        arr = self._kv4_on(desc, layers, "nodes")
         self._check(_lib.lumo_kv4_attention(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_publish(self, desc: "TreeDesc", layers, accepted: torch.Tensor, length: torch.Tensor,
                     ctx_len_out: Optional[torch.Tensor] = None, stream=None):
-        arr = self._kv4(layers)
+        arr = self._kv4_on(desc, layers)
         self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), int(accepted.shape[1]),
                                           _ptr(ctx_len_out), _stream(stream)))
 
@@ -685,7 +696,11 @@ class Kv4Layer:
             setattr(a, name, _ptr(self.tensors[name]))
         a.work_bytes = work.numel() * work.element_size() if work is not None else 0
         self.args = a
-        self.new_tokens = min((t.numel() // (int(Hkv) * 128) for t in (k_new, v_new) if t is not None), default=_ANY)
+        # what the tensors hold: words per sequence, tokens of the attention, tokens to write
+        room = lambda per, *tensors: min((t.numel() // max(per, 1) for t in tensors if t is not None), default=_ANY)       # noqa: E731
+        self.sequences = room(1, ctx_len, cache_row, status)
+        self.nodes = min(room(int(Hq) * 128, q, out), room(int(Hq), lse))
+        self.new_tokens = room(int(Hkv) * 128, k_new, v_new)
 
 
 class PageTable:

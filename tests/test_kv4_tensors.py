@@ -122,3 +122,36 @@ def test_packed_layers_keep_their_tensors(ctx):
     assert gone() is not None and len(packed) == 1
     with pytest.raises(ValueError, match="pack_kv4"):                     # an array of another making says nothing of its tensors
         ctx.kv4_append((B._Kv4Args * 1)(packed[0]), i32(1), i32(1))
+
+
+# ---- what a call on trees reads and writes ----
+def on_trees(**kw):
+    """A layer for two trees of three nodes, four query and two KV heads."""
+    t = dict(ctx_len=i32(2), cache_row=i32(2), status=i32(2), q=bf16(2, 3, 4, 128), k_new=bf16(2, 3, 2, 128), v_new=bf16(2, 3, 2, 128), out=bf16(2, 3, 4, 128),
+             lse=gpu(torch.zeros(2, 3, 4)), work=gpu(torch.zeros(64, dtype=torch.uint8)))
+    t.update(kw)
+    return B.Kv4Layer(**{**cache(), "Hq": 4}, **t)
+
+
+def test_the_layers_tensors_hold_what_the_trees_need(ctx):
+    desc = ctx.tree_desc(np.array([[-1, 0, 0]] * 2, dtype=np.int32))
+    acc, n = i32(2, 2), i32(2)
+    write, attend, publish = (lambda l: ctx.kv4_write_tree(desc, l), lambda l: ctx.kv4_attention(desc, l), lambda l: ctx.kv4_publish(desc, l, acc, n))
+    kept = gpu(torch.zeros(1 << 20, dtype=torch.uint8))
+    for good in (on_trees(work=kept), on_trees(work=kept, status=None, lse=None), on_trees(work=kept, ctx_len=i32(9), out=bf16(7, 4, 128))):
+        for call in (write, attend, publish):
+            for layers in ([good], ctx.pack_kv4([good])):
+                reaches_launch(lambda: call(layers))
+    small = {"ctx_len": (i32(1), "seq"), "cache_row": (i32(1), "seq"), "status": (i32(1), "seq"), "q": (bf16(5, 4, 128), "attn"), "out": (bf16(5, 4, 128), "attn"),
+             "lse": (gpu(torch.zeros(2, 3, 3)), "attn"), "k_new": (bf16(2, 2, 2, 128), "new"), "v_new": (bf16(5, 2, 128), "new")}
+    for name, (t, kind) in small.items():
+        layer = on_trees(**{name: t, "work": kept})
+        for layers in ([layer], ctx.pack_kv4([layer])):
+            for call, own in ((write, "new"), (attend, "attn"), (publish, "publish")):
+                if kind in ("seq", own):
+                    refused(lambda: call(layers), "too small")
+                else:
+                    reaches_launch(lambda: call(layers))
+    shared = {k: on_trees().tensors[k] for k in ("table", "ctx_len", "cache_row")}
+    two = [B.Kv4Layer(Hq=4, Hkv=2, page_size=16, **{**on_trees(work=kept).tensors, **shared, "out": o}) for o in (bf16(2, 3, 4, 128), bf16(2, 2, 4, 128))]
+    refused(lambda: attend(two), "too small")
