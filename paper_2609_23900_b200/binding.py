@@ -463,6 +463,9 @@ class Context:
     def kv4_publish(self, desc: "TreeDesc", layers, accepted: torch.Tensor, length: torch.Tensor,
                     ctx_len_out: Optional[torch.Tensor] = None, stream=None):
         arr = self._kv4_on(desc, layers)
+        if (accepted.dtype != torch.int32 or accepted.dim() != 2 or accepted.shape[0] < desc.B or length.dtype != torch.int32 or length.numel() < desc.B or
+                (ctx_len_out is not None and (ctx_len_out.dtype != torch.int32 or ctx_len_out.numel() < desc.B))):
+            raise ValueError("accepted must be int32 [B, lmax], length and ctx_len_out int32 [B]")
         self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), int(accepted.shape[1]),
                                           _ptr(ctx_len_out), _stream(stream)))
 

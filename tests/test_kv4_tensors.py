@@ -155,3 +155,14 @@ def test_the_layers_tensors_hold_what_the_trees_need(ctx):
     shared = {k: on_trees().tensors[k] for k in ("table", "ctx_len", "cache_row")}
     two = [B.Kv4Layer(Hq=4, Hkv=2, page_size=16, **{**on_trees(work=kept).tensors, **shared, "out": o}) for o in (bf16(2, 3, 4, 128), bf16(2, 2, 4, 128))]
     refused(lambda: attend(two), "too small")
+
+
+def test_publication_takes_int32_paths_of_every_tree(ctx):
+    desc = ctx.tree_desc(np.array([[-1, 0, 0]] * 2, dtype=np.int32))
+    layers = ctx.pack_kv4([on_trees()])
+    publish = lambda acc, n, out=None: lambda: ctx.kv4_publish(desc, layers, acc, n, out)     # noqa: E731
+    reaches_launch(publish(i32(2, 2), i32(2)))
+    reaches_launch(publish(i32(5, 3), i32(4), i32(2)))
+    for acc, n, out in ((i32(2, 2).long(), i32(2), None), (gpu(torch.zeros(2, 2)), i32(2), None), (i32(2, 2), i32(2).long(), None), (i32(2, 2), i32(2), i32(2).long()),
+                        (i32(1, 2), i32(2), None), (i32(4), i32(2), None), (i32(2, 2, 1), i32(2), None), (i32(2, 2), i32(1), None), (i32(2, 2), i32(2), i32(1))):
+        refused(publish(acc, n, out), "accepted")
