@@ -401,6 +401,8 @@ class Context:
     # ---- norm and rotation, the paged 4-bit cache ----
     def qk_norm_rope(self, layer: "QkNormRope", desc: Optional["TreeDesc"] = None, stream=None):
         """Norm of every query and key head and the position rotation, in one pass; with ``desc`` the tokens are its trees' nodes."""
+        if desc is not None and desc.B > layer.sequences:
+            raise ValueError("ctx_len must be [B], a length for each of the trees")
         self._check(_lib.lumo_qk_norm_rope(self._h, desc._h if desc is not None else None, layer.args, _stream(stream)))
 
     @staticmethod
@@ -661,6 +663,7 @@ class QkNormRope:
         for name in ("q_weight", "k_weight", "inv_freq", "pos", "ctx_len"):
             setattr(a, name, _ptr(self.tensors[name]))
         self.args = a
+        self.sequences = ctx_len.numel() if ctx_len is not None and pos is None and a.rot else _ANY      # whose lengths are read
 
 
 class Kv4Layer:

@@ -166,3 +166,17 @@ def test_publication_takes_int32_paths_of_every_tree(ctx):
     for acc, n, out in ((i32(2, 2).long(), i32(2), None), (gpu(torch.zeros(2, 2)), i32(2), None), (i32(2, 2), i32(2).long(), None), (i32(2, 2), i32(2), i32(2).long()),
                         (i32(1, 2), i32(2), None), (i32(4), i32(2), None), (i32(2, 2, 1), i32(2), None), (i32(2, 2), i32(1), None), (i32(2, 2), i32(2), i32(1))):
         refused(publish(acc, n, out), "accepted")
+
+
+def test_the_rotation_has_a_context_length_for_every_tree(ctx):
+    desc = ctx.tree_desc(np.array([[-1, 0, 0]] * 2, dtype=np.int32))
+    x, freq = bf16(2, 3, 4, 128), gpu(torch.zeros(64))
+    rope = lambda d=desc, **kw: lambda: ctx.qk_norm_rope(B.QkNormRope(q=x, q_out=x, **kw), d)                 # noqa: E731
+    reaches_launch(rope(inv_freq=freq, ctx_len=i32(2)))
+    reaches_launch(rope(inv_freq=freq, ctx_len=i32(5)))
+    reaches_launch(rope(inv_freq=freq, pos=i32(6), ctx_len=i32(1)))       # positions given: lengths are not read
+    reaches_launch(rope(inv_freq=freq, pos=i32(6), ctx_len=i32(1), d=None))
+    reaches_launch(rope(ctx_len=i32(1)))                                  # the norm alone
+    refused(rope(inv_freq=freq, ctx_len=i32(1)), "ctx_len")
+    with pytest.raises(B.LumoError, match="ctx_len"):
+        rope(inv_freq=freq)()
