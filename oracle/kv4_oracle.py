@@ -173,7 +173,7 @@ class Pages:
         for i, (s, d) in enumerate(zip(src, dst)):
             if s == -1 or d == -1:
                 continue
-            ok = 0 <= s < len(self.rows) and 0 <= d < len(self.rows) and d not in dst[:i] and s not in dst and d not in src
+            ok = 0 <= s < len(self.rows) and 0 <= d < len(self.rows) and d not in dst[:i] and d not in src
             if not ok or before[d]:
                 st[i] = SEQ_BAD_ROW
                 continue

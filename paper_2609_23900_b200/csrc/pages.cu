@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_free_kernel(const PageT
 
 // ---- fork ---------------------------------------------------------------------------------
 // A CTA per pair: the destination row, empty so far, gets the source's pages.  A destination that an earlier pair names, or that is
-// a source of the call, is refused, so no CTA reads what another one writes.
+// a source of the call, is refused, so no CTA reads what another one writes: a source that a pair names as its destination stays as it was.
 __global__ void __launch_bounds__(kCopyThreads) pages_fork_kernel(const PageTableDev t, const int32_t* src, const int32_t* dst, int n, int32_t* status) {
   const int i = blockIdx.x, tid = threadIdx.x;
   pdl_wait();          // everything below may belong to earlier kernels
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_fork_kernel(const PageTabl
   bool clash = false;
   for (int j = tid; j < n; j += kCopyThreads) {
     const int dj = dst[j];
-    clash |= (dj == d && j < i) || (dj == s) || (src[j] == d);
+    clash |= (dj == d && j < i) || src[j] == d;
   }
   clash = __syncthreads_or(clash);
   int have = 0;
