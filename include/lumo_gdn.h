@@ -545,7 +545,7 @@ int64_t lumo_pages_work_ints(int n_rows, int n_pages);
 /* Empty rows, all pages free (page 0 is taken first). */
 int lumo_pages_init(lumo_ctx* ctx, const lumo_page_table* t, void* stream);
 /* Row dst[i], which holds no pages, shares all pages of row src[i].  A dst that an earlier pair names, or that is a source of the call, is
- * refused. */
+ * refused.  A pair with -1 on either side is passed over and names nothing. */
 int lumo_pages_fork(lumo_ctx* ctx, const lumo_page_table* t, const int32_t* src, const int32_t* dst, int n, int32_t* status, void* stream);
 /* Makes positions [start[i], end[i]) of row rows[i] writable (end = NULL: end[i] = start[i] + add): pages among them that other rows share
  * are replaced by copies in all pools, missing ones up to end are added (with whatever bytes they hold).  When all sharers of a page
@@ -562,7 +562,7 @@ int lumo_pages_free(lumo_ctx* ctx, const lumo_page_table* t, const int32_t* rows
 int lumo_pages_compact(lumo_ctx* ctx, const lumo_page_table* t, void* stream);
 /* Rows of caches that are not paged (recurrent states, convolution histories): row src[i] of every block copied to row dst[i].  blocks:
  * HOST array of n_blocks (1 to 64) device arrays of n_rows rows, row_bytes[j] bytes each (HOST array; multiples of 16).  A dst that an
- * earlier pair names, or that is a source of the call, is refused; row -1 is passed over. */
+ * earlier pair names, or that is a source of the call, is refused; a pair with -1 on either side is passed over and names nothing. */
 int lumo_rows_copy(lumo_ctx* ctx, void* const* blocks, const int64_t* row_bytes, int n_blocks, int n_rows, const int32_t* src,
                    const int32_t* dst, int n, int32_t* status, void* stream);
 

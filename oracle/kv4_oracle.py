@@ -173,7 +173,9 @@ class Pages:
         for i, (s, d) in enumerate(zip(src, dst)):
             if s == -1 or d == -1:
                 continue
-            ok = 0 <= s < len(self.rows) and 0 <= d < len(self.rows) and d not in dst[:i] and d not in src
+            live = [(t, e) for t, e in zip(src, dst) if t != -1 and e != -1]                # (a pair that is passed over names nothing)
+            named = [e for t, e in zip(src[:i], dst[:i]) if t != -1]
+            ok = 0 <= s < len(self.rows) and 0 <= d < len(self.rows) and d not in named and all(t != d for t, _ in live)
             if not ok or before[d]:
                 st[i] = SEQ_BAD_ROW
                 continue

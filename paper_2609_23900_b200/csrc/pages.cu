@@ -267,6 +267,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_free_kernel(const PageT
 // ---- fork ---------------------------------------------------------------------------------
 // A CTA per pair: the destination row, empty so far, gets the source's pages.  A destination that an earlier pair names, or that is
 // a source of the call, is refused, so no CTA reads what another one writes: a source that a pair names as its destination stays as it was.
+// A pair that is passed over (-1 on either side) names nothing.
 __global__ void __launch_bounds__(kCopyThreads) pages_fork_kernel(const PageTableDev t, const int32_t* src, const int32_t* dst, int n, int32_t* status) {
   const int i = blockIdx.x, tid = threadIdx.x;
   pdl_wait();          // everything below may belong to earlier kernels
@@ -279,8 +280,8 @@ __global__ void __launch_bounds__(kCopyThreads) pages_fork_kernel(const PageTabl
   }
   bool clash = false;
   for (int j = tid; j < n; j += kCopyThreads) {
-    const int dj = dst[j];
-    clash |= (dj == d && j < i) || src[j] == d;
+    const int sj = src[j], dj = dst[j];
+    clash |= sj != -1 && dj != -1 && ((dj == d && j < i) || sj == d);
   }
   clash = __syncthreads_or(clash);
   int have = 0;
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(kCopyThreads) rows_copy_kernel(const PagePools
     const bool skip = s == -1 || d == -1;
     bool bad = s < 0 || s >= n_rows || d < 0 || d >= n_rows;
     if (!skip && !bad)
-      for (int j = 0; j < n; ++j) bad |= (dst_s[j] == d && j < i) || src_s[j] == d;
+      for (int j = 0; j < n; ++j) bad |= src_s[j] != -1 && dst_s[j] != -1 && ((dst_s[j] == d && j < i) || src_s[j] == d);
     ok_s[i] = !skip && !bad;
     if (status && blockIdx.x == 0 && blockIdx.y == 0) status[i] = !skip && bad ? (int)LUMO_SEQ_BAD_ROW : (int)LUMO_SEQ_OK;
   }

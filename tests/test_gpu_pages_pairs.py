@@ -1,5 +1,5 @@
 """Lists of pairs (pages forked, rows copied) by their contract: a destination that an earlier pair names, or that is a source of the call, is
-refused; everything else goes through.  Both calls judge one list alike."""
+refused; everything else goes through, and a pair with -1 on either side is as if it were not there.  Both calls judge one list alike."""
 import random
 
 import numpy as np
@@ -35,6 +35,10 @@ LISTS = {
     "chain": ([0, 1], [1, 5]),                              # 1 is a source: refused as a destination, and forked as it was
     "long_chain": ([0, 1, 2, 5], [1, 2, 5, 6]),
     "source_of_several": ([0, 0, 1, 2], [5, 6, 7, 0]),
+    "padding_names_no_destination": ([-1, 0], [5, 5]),
+    "padding_names_no_source": ([5, 0], [-1, 5]),
+    "padding_on_both_sides": ([-1, -1, 0, 1, -1], [-1, 5, 5, 6, 6]),
+    "all_padding": ([-1, 3, -1], [2, -1, -1]),
     "named_twice": ([0, 1, 2], [5, 5, 6]),
     "named_first_by_a_refused_pair": ([99, 0], [5, 5]),
     "onto_itself": ([0, 1], [0, 5]),
@@ -49,7 +53,7 @@ def test_both_calls_go_by_the_contract(name):
     else:
         rng = random.Random(name)
         n = rng.randint(1, 9)
-        src, dst = [rng.choice([0, 0, 1, 2, 3, 4, 7, 12]) for _ in range(n)], [rng.choice([5, 6, 7, 8, 9, 3]) for _ in range(n)]
+        src, dst = [rng.choice([-1, 0, 0, 1, 2, 3, 4, 7, 12]) for _ in range(n)], [rng.choice([-1, -1, 5, 6, 7, 8, 9, 3]) for _ in range(n)]
     want = verdict(src, dst)
     t = {k: i32(v) for k, v in dict(table=[[-7] * MAX_PAGES] * N_ROWS, row_pages=[0] * N_ROWS, refs=[0] * 20, free_list=[0] * 20, free_count=[0],
                                     work=[0] * binding.pages_work_ints(N_ROWS, 20)).items()}
