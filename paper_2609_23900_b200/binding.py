@@ -285,7 +285,7 @@ class Context:
         self._check(_lib.lumo_ctx_set_scan_algo(self._h, {"auto": 0, "rank1": 1, "gram": 2, "solve": 3, "direct": 4, "tensor": 5}[algo]))
 
     def set_timeout_drill(self, on: bool):
-        """Test aid: the tensor-core scan issues no tensor-core work, so its bounded wait runs out."""
+        """Test aid: the tensor-core scans and the 4-bit attention issue nothing asynchronous, so their bounded waits run out."""
         self._check(_lib.lumo_ctx_set_timeout_drill(self._h, int(on)))
 
     def set_overlap(self, on: bool = True):

@@ -245,7 +245,7 @@ int lumo_kv4_attention(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4
     const Kv4AttnPtrs p = {a.pages, a.q, a.out, a.lse, a.status};
     Kv4Plan plan;
     kv4_plan(s, p, desc->d_vis, desc->d_slot_used, a.scale, a.q_stride ? a.q_stride : (long long)a.Hq * 128, a.out_dtype == LUMO_BF16, a.n_splits, a.work,
-             ctx->sm_count, &plan);
+             ctx->sm_count, ctx->timeout_drill, &plan);
     cudaError_t e = timed(ctx, LUMO_K_KV4_ATTN, st, [&] { return launch_kv4_attn(plan, ctx->overlap, st); });
     if (e != cudaSuccess) return cuda_fail(ctx, e, "4-bit attention launch");
     e = timed(ctx, LUMO_K_KV4_MERGE, st, [&] { return launch_kv4_merge(plan, ctx->overlap, st); });

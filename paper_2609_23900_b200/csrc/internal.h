@@ -57,7 +57,7 @@ struct lumo_ctx {
   cudaStream_t setup = nullptr; // set-up copies, waited for by the call that makes them (created by the first)
   // optional per-launch timing (lumo_ctx_timing_*): a fixed pool of event pairs
   int scan_algo = 0;            // 0 auto, 1 rank-1, 2 Gram form with forward substitution, 3 solved Gram form, 4 Gram form with closed-form tail, 5 the same with the output sum on the tensor core
-  bool timeout_drill = false;   // test aid: the solved and the streamed scan skip their tensor-core work (lumo_ctx_set_timeout_drill)
+  bool timeout_drill = false;   // test aid: the solved and the streamed scan and the 4-bit attention skip their asynchronous work (lumo_ctx_set_timeout_drill)
   bool overlap = true;          // kernels are launched as programmatic dependents of the kernel before them
   lumo::CallOrder order;        // what is in front of a call in its stream: decides what may be read ahead of a dependency wait
   bool timing = false;
@@ -425,10 +425,10 @@ struct Kv4AttnArgs {
   float scale_log2;                                   // scale * log2(e) * 2^k_exp
   float v_mul;                                        // 2^v_exp
 };
-struct Kv4Plan { Kv4AttnArgs a; int sms; };
+struct Kv4Plan { Kv4AttnArgs a; int sms; bool drill; };      // drill: nothing asynchronous is issued, the waits run out (lumo_ctx_set_timeout_drill)
 size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms);
 void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
-              int n_splits, void* work, int sms, Kv4Plan* plan);
+              int n_splits, void* work, int sms, bool drill, Kv4Plan* plan);
 cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st);
 cudaError_t launch_kv4_attn_tc(const Kv4Plan& plan, bool pdl, cudaStream_t st);   // R = 128 (kv4_attn_tc.cu)
 cudaError_t launch_kv4_merge(const Kv4Plan& plan, bool pdl, cudaStream_t st);

@@ -75,9 +75,10 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return r;
 }
 
-template <int NT>
+template <int NT, bool kDrill>
 __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(const Kv4AttnArgs a) {
   using C = Small<NT>;
+  auto wait = [](unsigned long long* bar, uint32_t parity) { return mbar_wait(bar, parity, kDrill ? kSpinLimitDrill : kSpinLimit); };
   extern __shared__ __align__(128) unsigned char smem[];
   typename C::Ctl& sm = *reinterpret_cast<typename C::Ctl*>(smem + C::kOffCtl);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -107,18 +108,19 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
         const uint32_t st = it % C::kStages, use = it / C::kStages;
         const bool wanted = walk.wanted(j);
         const int pg = walk.take(j);
-        if (use > 0 && ok) ok = mbar_wait(&sm.empty[st], (use - 1) & 1u);
+        if (use > 0 && ok) ok = wait(&sm.empty[st], (use - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (j == 0 && lane == 0) sm.bad_page[nseg & 15u] = 0;
-        load_tile<true>(a, sg, wanted, pg, 0, smem_u32(smem) + st * kTileBytes, &sm.full[it % (2 * C::kStages)], &sm.bad_page[nseg & 15u], policy);
+        if (!kDrill)
+          load_tile<true>(a, sg, wanted, pg, 0, smem_u32(smem) + st * kTileBytes, &sm.full[it % (2 * C::kStages)], &sm.bad_page[nseg & 15u], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
     }
     if (!ok && lane == 0) sm.timed_out = 1;
     // no copy may be on its way when the CTA leaves: the last use of every barrier (complete already unless a wait ran out)
-    for (uint32_t s = 0; s < 2 * C::kStages && s < it; ++s) mbar_wait(&sm.full[s], ((it - 1 - s) / (2 * C::kStages)) & 1u);
+    for (uint32_t s = 0; s < 2 * C::kStages && s < it; ++s) wait(&sm.full[s], ((it - 1 - s) / (2 * C::kStages)) & 1u);
   } else {
     // ---------------- consumers ----------------
     const int g = lane >> 2, t = lane & 3;
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
       for (int gi = warp; gi < sg.n * C::kPieces; gi += C::kWarps) {
         const uint32_t tt = it + gi / C::kPieces, st = tt % C::kStages;
         const int first = (gi % C::kPieces) * 16 * C::kSub;
-        if (ok) ok = mbar_wait(&sm.full[tt % (2 * C::kStages)], (tt / (2 * C::kStages)) & 1u);
+        if (ok) ok = wait(&sm.full[tt % (2 * C::kStages)], (tt / (2 * C::kStages)) & 1u);
         ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
         const int pos0 = (sg.t0 + gi / C::kPieces) * kKeys + first;     // the piece's first position
         if (ok && pos0 < sg.ctx + a.Ns) {
@@ -337,7 +339,7 @@ __global__ void __launch_bounds__(Small<NT>::kThreads, 1) kv4_attn_small_kernel(
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.empty[st]);
+        if (ok && lane == 0) mbar_arrive(&sm.empty[st]); // (whoever gave up keeps the stage: its copies may not have landed, and none go on top)
       }
       it += sg.n;
       // ---- the warps' parts meet: maxima and sums, then the outputs of eight rows at a time
@@ -521,18 +523,18 @@ __global__ void __launch_bounds__(256, 4) kv4_merge_kernel(const Kv4AttnArgs a, 
   if (a.lse && cg == 0) a.lse[row] = lse;
 }
 
-template <int NT>
+template <int NT, bool kDrill>
 cudaError_t launch_small(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   static bool configured[kMaxDevices] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 0 && dev < kMaxDevices && !configured[dev]) {
-    e = cudaFuncSetAttribute(kv4_attn_small_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Small<NT>::kBytes);
+    e = cudaFuncSetAttribute(kv4_attn_small_kernel<NT, kDrill>, cudaFuncAttributeMaxDynamicSharedMemorySize, Small<NT>::kBytes);
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  return launch_kernel(kv4_attn_small_kernel<NT>, dim3(plan.a.C), dim3(Small<NT>::kThreads), Small<NT>::kBytes, st, pdl, plan.a);
+  return launch_kernel(kv4_attn_small_kernel<NT, kDrill>, dim3(plan.a.C), dim3(Small<NT>::kThreads), Small<NT>::kBytes, st, pdl, plan.a);
 }
 
 // Rows of a row tile: the register form up to sixteen, the tensor-memory form (kv4_attn_tc.cu) beyond.  The latter's 128-row tile costs the same
@@ -558,7 +560,7 @@ size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms) {
 }
 
 void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
-              int n_splits, void* work, int sms, Kv4Plan* plan) {
+              int n_splits, void* work, int sms, bool drill, Kv4Plan* plan) {
   Kv4AttnArgs& a = plan->a;
   a.pages = reinterpret_cast<const unsigned char*>(p.pages); a.q = p.q; a.out = p.out; a.lse = p.lse; a.status = p.status;
   a.ctx_len = s.ctx_len; a.cache_row = s.cache_row; a.table = s.table; a.vis = vis; a.used = used; a.q_stride = q_stride;
@@ -570,6 +572,7 @@ void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, cons
   const size_t slots = n_splits > 0 ? ctas : units + ctas;
   a.S = n_splits; a.C = (int)ctas; a.out_bf16 = out_bf16;
   plan->sms = sms;
+  plan->drill = drill;
   a.scale_log2 = ldexpf(scale * kLog2e, s.k_exp);
   a.v_mul = ldexpf(1.f, s.v_exp);
   unsigned char* w = reinterpret_cast<unsigned char*>(work);
@@ -581,7 +584,8 @@ void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, cons
 
 cudaError_t launch_kv4_attn(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   if (plan.a.R == 128) return launch_kv4_attn_tc(plan, pdl, st);
-  return plan.a.R == 8 ? launch_small<1>(plan, pdl, st) : launch_small<2>(plan, pdl, st);
+  if (plan.drill) return plan.a.R == 8 ? launch_small<1, true>(plan, pdl, st) : launch_small<2, true>(plan, pdl, st);
+  return plan.a.R == 8 ? launch_small<1, false>(plan, pdl, st) : launch_small<2, false>(plan, pdl, st);
 }
 
 // Four threads an entry while all of their CTAs run at once: then the chain of flights is what the merge takes (a token at 4k: 3.7 us, 4.6

@@ -18,7 +18,7 @@ constexpr int kTileBytes = kKeys * 2 * kKv4Entry;   // 18432: keys and values, c
 constexpr int kSeqCache = 64;         // sequences whose context length, cache row and tile count are kept in shared memory
 constexpr float kLag = 8.f;           // the reference maximum moves when exceeded by more than this (log2 units)
 constexpr float kLift = 6.f;          // probabilities are held as 2^kLift times themselves: at most 2^14 in f16, and what f16 drops is below 2^-30
-constexpr uint32_t kSpinLimit = 1u << 22;
+constexpr uint32_t kSpinLimit = 1u << 22, kSpinLimitDrill = 1u << 10;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -32,10 +32,10 @@ __device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, uint32_t
 __device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory");
 }
-// Bounded wait: false if the phase did not complete within the spin limit.
-__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity) {
+// Bounded wait: false if the phase did not complete within `limit` polls.
+__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity, uint32_t limit) {
   const uint32_t addr = smem_u32(bar);
-  for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+  for (uint32_t spin = 0; spin < limit; ++spin) {
     uint32_t done;
     asm volatile(
         "{\n.reg .pred p;\n"

@@ -161,7 +161,9 @@ __device__ __forceinline__ unsigned long long visible64(const uint32_t* row, int
   return v;
 }
 
+template <bool kDrill>
 __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnArgs a) {
+  auto wait = [](unsigned long long* bar, uint32_t parity) { return mbar_wait(bar, parity, kDrill ? kSpinLimitDrill : kSpinLimit); };
   extern __shared__ __align__(1024) unsigned char smem[];
   Ctl& sm = *reinterpret_cast<Ctl*>(smem + kOffCtl);
   const uint32_t sbase = smem_u32(smem);
@@ -211,35 +213,35 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         const uint32_t st = it % kStages, use = it / kStages;
         const bool wanted = walk.wanted(j);
         const int pg = walk.take(j);
-        if (use > 0 && ok) ok = mbar_wait(&sm.raw_empty[which][st], (use - 1) & 1u);
+        if (use > 0 && ok) ok = wait(&sm.raw_empty[which][st], (use - 1) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (j == 0 && lane == 0) sm.bad_page[which][nseg & 15u] = 0;
-        load_tile<false>(a, sg, wanted, pg, which, sbase + kOffRaw + (which * kStages + st) * kRawBytes, &sm.raw_full[which][st],
+        if (!kDrill) load_tile<false>(a, sg, wanted, pg, which, sbase + kOffRaw + (which * kStages + st) * kRawBytes, &sm.raw_full[which][st],
                          &sm.bad_page[which][nseg & 15u], policy);
       }
       if (!ok) break;
       if (sg.n > 0) ++nseg;
     }
     // no copy may be on its way when the CTA leaves: the last use of every stage (complete already unless a wait ran out)
-    for (uint32_t s = 0; s < kStages && s < it; ++s) mbar_wait(&sm.raw_full[which][s], ((it - 1 - s) / kStages) & 1u);
+    for (uint32_t s = 0; s < kStages && s < it; ++s) wait(&sm.raw_full[which][s], ((it - 1 - s) / kStages) & 1u);
     if (!ok && lane == 0) sm.timed_out = 1u;
   } else if (warp == kIssueWarp) {
     // ---------------- issuer of S = Q K^T: both K-major, 128 rows of 128 B per dh half ----------------
-    // (whole warps run these loops, and one lane issues)
+    // (whole warps run these loops, and one lane issues; all lanes take part in electing it, also when a wait has run out for some)
     constexpr uint32_t id = umma_idesc(kRows, kKeys, 0);
     const uint64_t dq = umma_desc(sbase + kOffQ, 16, 1024), dk = umma_desc(sbase + kOffK, 16, 1024);
     while (work.next(&sg)) {
       if (sg.n == 0) continue;
-      if (ok) ok = mbar_wait(&sm.q_full, nseg & 1u);
+      if (ok) ok = wait(&sm.q_full, nseg & 1u);
       for (int j = 0; j < sg.n; ++j, ++it) {
-        if (ok) ok = mbar_wait(&sm.k_full[it & 1u], (it >> 1) & 1u);
+        if (ok) ok = wait(&sm.k_full[it & 1u], (it >> 1) & 1u);
         // tile t's S buffer is free when tile t - 3's probabilities have been used
-        if (it >= kBufs && ok) ok = mbar_wait(&sm.o_done[it % kBufs], (it / kBufs - 1) & 1u);
+        if (it >= kBufs && ok) ok = wait(&sm.o_done[it % kBufs], (it / kBufs - 1) & 1u);
         tc_fence_after();
         const uint64_t kd = dk + (it & 1u) * (kOpBytes >> 4);
         const uint32_t d = tmem + (it % kBufs) * kKeys;
-        if (ok && elect_one()) {
+        if (elect_one() && ok && !kDrill) {
 #pragma unroll
           for (int ks = 0; ks < kDh / 16; ++ks) {
             constexpr int half16 = kHalfBytes >> 4;
@@ -251,11 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       }
       ++nseg;
     }
-    if (!ok) {                        // products may still run: they end before tensor memory is freed
-      if (elect_one()) umma_commit(&sm.drain[0]);
-      mbar_wait(&sm.drain[0], 0);
-      if (lane == 0) sm.timed_out = 1u;
-    }
+    if (!ok) sm.timed_out = 1u;
   } else if (warp == kIssueWarp + 1) {
     // ---------------- issuer of O += P V ----------------
     // A = P in the first half of its S buffer, B = V tile (MN-major: 128 B of dh per key row, the two dh halves kHalfBytes apart, 16 keys =
@@ -265,12 +263,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
     while (work.next(&sg)) {
       if (sg.n == 0) continue;
       for (int j = 0; j < sg.n; ++j, ++it) {
-        if (j == 0 && nseg > 0 && ok) ok = mbar_wait(&sm.o_free, (nseg - 1) & 1u);
-        if (ok) ok = mbar_wait(&sm.pv_full[it % kBufs], (it / kBufs) & 1u);
+        if (j == 0 && nseg > 0 && ok) ok = wait(&sm.o_free, (nseg - 1) & 1u);
+        if (ok) ok = wait(&sm.pv_full[it % kBufs], (it / kBufs) & 1u);
         tc_fence_after();
         const uint64_t vd = dv + (it & 1u) * (kOpBytes >> 4);
         const uint32_t p = tmem + (it % kBufs) * kKeys;
-        if (ok && elect_one()) {
+        if (elect_one() && ok && !kDrill) {
 #pragma unroll
           for (int ks = 0; ks < kKeys / 16; ++ks) umma_ta(tmem + kColO, p + ks * 8, vd + ks * (2048 >> 4), id, (j == 0 && ks == 0) ? 0u : 1u);
           umma_commit(&sm.o_done[it % kBufs]);
@@ -279,11 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       }
       ++nseg;
     }
-    if (!ok) {
-      if (elect_one()) umma_commit(&sm.drain[1]);
-      mbar_wait(&sm.drain[1], 0);
-      if (lane == 0) sm.timed_out = 1u;
-    }
+    if (!ok) sm.timed_out = 1u;
   } else if (warp >= kSoftmaxWarps) {
     // ---------------- codes to operands: keys (which = 0) or values (1) ----------------
     const int which = (warp - kSoftmaxWarps) >> 2, w = warp & 3;
@@ -298,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         const int pos0 = (sg.t0 + j) * kKeys;
         const bool tail = pos0 + kKeys > sg.ctx;         // uniform: the tile reaches past the committed context
         const unsigned char* raw = smem + kOffRaw + (which * kStages + st) * kRawBytes;
-        if (ok) ok = mbar_wait(&sm.raw_full[which][st], (it / kStages) & 1u);
+        if (ok) ok = wait(&sm.raw_full[which][st], (it / kStages) & 1u);
         ok = __all_sync(0xffffffffu, ok);                // (what follows shuffles: all lanes or none)
         uint4 code[4];
         uint32_t sc[4];
@@ -312,11 +306,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.raw_empty[which][st]);  // (the codes are in registers)
+        // (the codes are in registers; whoever gave up keeps the stage: its copies may not have landed, and none go on top)
+        if (ok && lane == 0) mbar_arrive(&sm.raw_empty[which][st]);
         // the operand buffer is free when the product two tiles back has read it (that of a K tile is announced by its logits)
         if (it >= 2 && ok) {
           const uint32_t b2 = (it - 2) % kBufs;
-          ok = mbar_wait(which ? &sm.o_done[b2] : &sm.s_full[b2], ((it - 2) / kBufs) & 1u);
+          ok = wait(which ? &sm.o_done[b2] : &sm.s_full[b2], ((it - 2) / kBufs) & 1u);
         }
         ok = __all_sync(0xffffffffu, ok);
         if (ok) {
@@ -438,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
         if ((int)buf != half) continue;                  // the other group's tile
         const int kpos0 = (sg.t0 + j) * kKeys;
         const bool tail = kpos0 + kKeys > sg.ctx;        // uniform: the tile reaches past the committed context
-        if (ok) ok = mbar_wait(&sm.s_full[sb], (it / kBufs) & 1u);
+        if (ok) ok = wait(&sm.s_full[sb], (it / kBufs) & 1u);
         tc_fence_after();
         __syncwarp();
         if (warp_ok) {
@@ -485,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
             if (j > 0 && __any_sync(0xffffffffu, mnew != cur && cur != -INFINITY)) {
               // O still takes the product of the tile before: wait for it, then scale this row of it
               const float corr = cur == -INFINITY ? 1.f : ex2(cur - mnew);
-              if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
+              if (ok) ok = wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
               tc_fence_after();
               __syncwarp();
 #pragma unroll 1
@@ -526,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
           l = ls[0].x + ls[0].y;
           tmem_st_wait();
           if (tail) {                                    // NaN values among the keys this row sees
-            if (ok) ok = mbar_wait(&sm.v_full[sb], (it / kBufs) & 1u);
+            if (ok) ok = wait(&sm.v_full[sb], (it / kBufs) & 1u);
             uint32_t any = 0;
 #pragma unroll 4
             for (int c = 0; c < 32; ++c) any |= sm.nan_blocks[buf][c];
@@ -548,8 +543,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
       pair_sync(pair_bar);
       // (behind the barrier: the last tile's logits are known to be there, hence the product three tiles before, whose phase this wait
       // would otherwise take for the last one's)
-      if (ok) ok = mbar_wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
+      if (ok) ok = wait(&sm.o_done[(it - 1) % kBufs], ((it - 1) / kBufs) & 1u);
       tc_fence_after();
+      __syncwarp();
       // (behind the wait: the last tile has been loaded; both loaders see the same pages)
       const bool bad = *reinterpret_cast<volatile uint32_t*>(&sm.bad_page[0][nseg & 15u]) != 0;
       const float mine = m;
@@ -616,23 +612,35 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
 
   tc_fence_before();
   __syncthreads();
+  if (sm.timed_out) {                 // products may still run that nobody awaited: they end before tensor memory is freed
+    if (warp >= kIssueWarp) {
+      if (elect_one()) umma_commit(&sm.drain[warp - kIssueWarp]);
+      wait(&sm.drain[warp - kIssueWarp], 0);
+    }
+    __syncthreads();
+  }
   if (tid == 0) a.cta_code[blockIdx.x] = (int)sm.timed_out;      // the merge kernel turns this into status words
   if (warp == kIssueWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
 }  // namespace
 
-cudaError_t launch_kv4_attn_tc(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+template <bool kDrill>
+static cudaError_t launch_tc(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   static bool configured[kMaxDevices] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 0 && dev < kMaxDevices && !configured[dev]) {
-    e = cudaFuncSetAttribute(kv4_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    e = cudaFuncSetAttribute(kv4_attn_tc_kernel<kDrill>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  return launch_kernel(kv4_attn_tc_kernel, dim3(plan.a.C), dim3(kThreads), kSmemBytes, st, pdl, plan.a);
+  return launch_kernel(kv4_attn_tc_kernel<kDrill>, dim3(plan.a.C), dim3(kThreads), kSmemBytes, st, pdl, plan.a);
+}
+
+cudaError_t launch_kv4_attn_tc(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
+  return plan.drill ? launch_tc<true>(plan, pdl, st) : launch_tc<false>(plan, pdl, st);       // (the kernel in use does not carry the test aid)
 }
 
 }  // namespace lumo
