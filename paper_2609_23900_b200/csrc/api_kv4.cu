@@ -226,9 +226,9 @@ int lumo_kv4_attention(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv4
   if (!(a0.scale > 0.f)) return fail(ctx, LUMO_ERR_ARG, "scale must be positive");
   if (a0.out_dtype != LUMO_F32 && a0.out_dtype != LUMO_BF16) return fail(ctx, LUMO_ERR_UNSUPPORTED, "out_dtype must be f32 or bf16");
   if (a0.n_splits < 0 || a0.n_splits > 32) return fail(ctx, LUMO_ERR_ARG, "n_splits must be 0 (automatic) or in [1, 32]");
-  // the kernels count key tiles of all (sequence, KV head, row tile) units in 32 bits
-  const double units = (double)s.B * s.Hkv * ((double)(s.Hq / s.Hkv) * s.N / 8 + 1);
-  if (units * ((double)s.max_pages * s.page / 128 + 8) >= 2147483648.0 || units * 32 >= 2147483648.0)
+  // The kernels number the key tiles of all (sequence, KV head, row tile) units in 32 bits (and add a CTA's share to a position: hence not
+  // quite 2^31), and so they do the slots, 32 to a unit at most.
+  if (kv4_line(s) > 2000000000LL || kv4_units(s.B, s.N, s.Hq, s.Hkv) * 32 > INT_MAX)
     return fail(ctx, LUMO_ERR_UNSUPPORTED, "batch x KV heads x positions too large for one call");
   const size_t need = kv4_work_bytes(s.B, s.N, s.Hq, s.Hkv, a0.n_splits, ctx->sm_count);
   for (int l = 0; l < n_layers; ++l) {

@@ -426,6 +426,10 @@ struct Kv4AttnArgs {
   float v_mul;                                        // 2^v_exp
 };
 struct Kv4Plan { Kv4AttnArgs a; int sms; bool drill; };      // drill: nothing asynchronous is issued, the waits run out (lumo_ctx_set_timeout_drill)
+// Units of a call, and the longest line their tiles and the idle positions in front of them can make (kv4_attn.h numbers both in 32 bits).
+long long kv4_units(int B, int N, int Hq, int Hkv);
+long long kv4_line(const Kv4Shape& s);
+int kv4_segment_cost_tc();                            // idle positions a unit of the tensor-memory form is charged
 size_t kv4_work_bytes(int B, int N, int Hq, int Hkv, int n_splits, int sms);
 void kv4_plan(const Kv4Shape& s, const Kv4AttnPtrs& p, const uint32_t* vis, const uint32_t* used, float scale, long long q_stride, int out_bf16,
               int n_splits, void* work, int sms, bool drill, Kv4Plan* plan);

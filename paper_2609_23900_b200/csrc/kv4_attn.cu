@@ -545,9 +545,15 @@ int rows_per_tile(int G, int N) { return G * N <= 8 ? 8 : G * N <= 16 ? 16 : 128
 
 }  // namespace
 
-static long long kv4_units(int B, int N, int Hq, int Hkv) {
+long long kv4_units(int B, int N, int Hq, int Hkv) {
   const int G = Hq / Hkv, R = rows_per_tile(G, N);
   return (long long)B * Hkv * ((G * N + R - 1) / R);
+}
+long long kv4_line(const Kv4Shape& s) {
+  const int R = rows_per_tile(s.Hq / s.Hkv, s.N);
+  const int cost = R == 8 ? Small<1>::W::kSegmentCost : R == 16 ? Small<2>::W::kSegmentCost : kv4_segment_cost_tc();
+  const long long tiles = (((long long)s.max_pages << s.page_log2) + kKeys - 1) / kKeys;
+  return kv4_units(s.B, s.N, s.Hq, s.Hkv) * (tiles + cost);
 }
 
 // workspace: partial outputs [slots][R][128], log-sum-exps [slots][R], CTA codes, the units' slots

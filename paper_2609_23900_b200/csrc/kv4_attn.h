@@ -95,7 +95,7 @@ struct Segment {
 };
 struct WorkState {
   int b, q;           // current sequence, unit within the sequence
-  int g, g_end;       // next position on the line, end of this CTA's share (the host bounds the line below 2^31)
+  int g, g_end;       // next position on the line, end of this CTA's share (the host bounds the line: kv4_line)
   int g_unit;         // position at which the current unit's stretch (idle prefix, then its tiles) starts
   int nt;             // tiles per unit of the current sequence
   int per;            // automatic mode: positions per CTA
@@ -116,6 +116,7 @@ __device__ __forceinline__ int seq_tiles(const Kv4AttnArgs& a, int cx, int cr) {
 
 template <int kCost, int kMinTiles, int kSlack>
 struct Work : WorkState {
+  static constexpr int kSegmentCost = kCost;
   const Kv4AttnArgs& a;
   const SeqCache& sc;
   bool fresh = true;

@@ -625,6 +625,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attn_tc_kernel(const Kv4AttnA
 
 }  // namespace
 
+int kv4_segment_cost_tc() { return TcWork::kSegmentCost; }
+
 template <bool kDrill>
 static cudaError_t launch_tc(const Kv4Plan& plan, bool pdl, cudaStream_t st) {
   static bool configured[kMaxDevices] = {};
