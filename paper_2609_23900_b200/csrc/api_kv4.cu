@@ -174,7 +174,7 @@ int lumo_kv4_write_tree(lumo_ctx* ctx, const lumo_tree_desc* desc, const lumo_kv
   cudaStream_t st = (cudaStream_t)stream;
   const Kv4Layers L = kv4_views(layers, n_layers);
   ctx->order.begin(ctx->device, stream);
-  cudaError_t e = timed(ctx, LUMO_K_KV4_WRITE, st, [&] { return launch_kv4_write(L, s, n_layers, ctx->sm_count, ctx->overlap, st); });
+  cudaError_t e = timed(ctx, LUMO_K_KV4_WRITE, st, [&] { return launch_kv4_write(L, s, n_layers, ctx->overlap, st); });
   return launched(ctx, e, CallOrder::kOther, "4-bit write launch");
 }
 

@@ -404,7 +404,7 @@ inline FewKv4Layers few_layers(const Kv4Layers& L) {
 }
 // tokens listed one by one: T of them, rows and positions on the device; status may be null
 struct Kv4Tokens { int T; const int32_t* row; const int32_t* pos; int32_t* status; };
-cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, int sms, bool pdl, cudaStream_t st);
+cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, bool pdl, cudaStream_t st);
 cudaError_t launch_kv4_append(const Kv4Layers& L, const Kv4Shape& s, int n_layers, const Kv4Tokens& t, int sms, bool pdl, cudaStream_t st);
 cudaError_t launch_kv4_read(const void* pages, const Kv4Shape& s, const Kv4Tokens& t, void* k_out, void* v_out, int sms,
                             bool pdl, cudaStream_t st);

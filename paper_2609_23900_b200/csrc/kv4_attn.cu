@@ -4,8 +4,10 @@
 //
 // Keys and values come as e2m1 codes and e4m3 scales, 144 bytes a position and KV head.  A code times its scale has at most six
 // significant bits, so it is exact in f16: the tensor cores multiply f16 operands whose only roundings are those of the
-// probabilities (2^-12 relative each).  A query row is scaled by a power of two to fit f16 (its elements are bf16: eight bits) and the logits
-// are scaled back in fp32; sums are fp32.
+// probabilities (half a step: 2^-11 relative each).  Against the same formula with fp32 probabilities, bf16 outputs differ by 0.0005 to 0.0009
+// of their norm (neighbouring bf16 numbers here and there; the bf16 rounding itself is 0.0017); fp32 ones would cost the second product twice
+// over (high and low parts).  A query row is scaled by a power of two to fit f16 (its elements are bf16: eight bits) and the logits are
+// scaled back in fp32; sums are fp32.
 //
 // The work is the list of 128-key tiles of all (sequence, KV head, row tile) units in order; a CTA takes a contiguous share of the list, and
 // every piece of its share that lies in one unit is a SEGMENT, whose normalised output and base-2 log-sum-exp go to a slot;
@@ -36,8 +38,8 @@ namespace {
 //
 // Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
 // A tile takes each scheduler 720 instructions (90 for 16 keys and scheduler; three quarters turn codes into f16), and the SM's share of the
-// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 55.6 us, 4.2 TB/s;
-// one token at 4k: 12.1 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
+// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 56 to 59 us, 4.0 TB/s;
+// one token at 4k: 12.2 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
 // merge the rest.
 template <int NT> struct Small {
   static constexpr int kWarps = NT == 1 ? 15 : 11;       // consumers; with the loader a multiple of four: 128 registers a thread, 168 for NT = 2
@@ -58,8 +60,9 @@ template <int NT> struct Small {
     uint32_t bad_page[16];                               // by segment number mod 16: the loader is never that far ahead
   };
   static constexpr int kBytes = kOffCtl + (int)sizeof(Ctl);
-  // A segment costs about as much as twelve tiles (sixteen tokens at 16k, one at 4k: 55.6 and 12.1 us; charged five 59 and 12.7, charged
-  // sixteen 57.8 and 12.4); no share below two tiles (four: 12.7 at 4k), and whole units up to three tiles longer than a share.
+  // A segment costs about as much as twelve tiles.  Charged 6, 12, 18, us: 16 tokens at 16k 58.5, 57.1, 59.8; one at 4k 12.4, 12.4, 12.5; 5
+  // at 30k 38.5, 36.8, 37.5; 9 trees of 2 nodes at 7k 27.7, 26.1, 26.8; 12 rows, 6 at 12k 40.1, 39.1, 40.7; 16 rows, 16 at 16k 95.2, 93.8,
+  // 97.5.  No share below two tiles (four: one at 4k takes 0.6 us more), and whole units up to three tiles longer than a share.
   using W = Work<12, 2, 3>;
 };
 static_assert(Small<1>::kBytes <= 227 * 1024 && Small<2>::kBytes <= 227 * 1024, "one CTA per SM");

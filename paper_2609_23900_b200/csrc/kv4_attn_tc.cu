@@ -22,8 +22,8 @@
 // each scheduler issues 1390 instructions: no unit is full, but five warps a scheduler find something to issue in three cycles of four at
 // best.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the memory.  Around the tiles a CTA spends 10 thousand cycles
 // until its first logits (lengths, page numbers, first copies and first instructions, one after another) and 4 to 6 thousand on the
-// read-out.  Measured, with the merge: 4 x 8 nodes at 8k 26.5 us, 8 x 28 at 16k 69 us (680 TFLOP/s), 64 nodes at 128k 161 us (850 TFLOP/s, at
-// 1.64 GHz under the power limit).
+// read-out.  Measured, with the merge: 4 x 8 nodes at 8k 26.5 to 27.5 us, 8 x 28 at 16k 71 to 77 us (615 to 665 TFLOP/s, at the power limit's
+// edge; 66 in a short run), 64 nodes at 128k 162 us (845 TFLOP/s, at 1.64 GHz under the power limit).
 #include "f32x2.h"
 #include "kv4_attn.h"
 
@@ -67,7 +67,8 @@ struct Ctl {
 };
 constexpr int kSmemBytes = kOffCtl + (int)sizeof(Ctl);
 static_assert(kSmemBytes + 1024 <= 227 * 1024, "one CTA per SM");
-// A segment's start and end cost about as much as eight tiles (8 x 28 nodes at 16k: 67.6 to 70 us, charged five: 71, three: 73 to 75).
+// A segment's start and end cost about as much as eight tiles.  Charged 4, 8, 12, us, in one short run: 8 x 28 nodes at 16k 67.4, 66.4, 68.1; 4
+// x 8 at 8k 28.8, 27.4, 28.4; 3 x 20 at 5k 21.8, 22.1, 22.7; 12 x 16 at 16k 88.0, 88.2, 90.9; 2 x 64 at 40k 77.8, 76.2, 76.9.
 using TcWork = Work<8, 4, 4>;
 
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }

@@ -10,8 +10,10 @@
 // does, and no division is needed.
 // Likewise c * s has at most six significant bits: reading back in bf16 is exact.
 //
-// Sixteen lanes a row of 128 numbers, 16 bytes of bf16 a lane.  At a prompt's size the instructions bound it, not the bytes: some 110 for two
-// rows to quantise and store, 70 to read back (8191 tokens of 8 heads, both ways: 23.6 us, 3.6 TB/s); a tree's entries take a launch.
+// Sixteen lanes a row of 128 numbers, 16 bytes of bf16 a lane.  At a prompt's size neither the bytes nor the instructions (110 for two rows to
+// quantise and store, 70 to read back) fill their units: 0.5 issued a cycle and scheduler with 40 % of the warps, most stalls on loads, and in
+// the read on the barrier behind which the places are known.  Latency bounds it (8191 tokens of 8 heads, both ways: 23.6 us, 3.6 TB/s); a
+// tree's entries take a launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) kv4_publish_kernel(const KL L, const
 
 }  // namespace
 
-cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, int, bool pdl, cudaStream_t st) {
+cudaError_t launch_kv4_write(const Kv4Layers& L, const Kv4Shape& s, int n_layers, bool pdl, cudaStream_t st) {
   const dim3 grid(s.N, s.B, n_layers);
   if (n_layers <= kFewLayers) return launch_kernel(kv4_write_kernel<FewKv4Layers>, grid, dim3(kThreads), 0, st, pdl, few_layers(L), s);
   return launch_kernel(kv4_write_kernel<Kv4Layers>, grid, dim3(kThreads), 0, st, pdl, L, s);

@@ -7,10 +7,11 @@
 // for two rows of 128, angles included).  A row (one head of one token) is held by dh / 8 lanes, so that both elements of a pair are in one
 // lane; sums and products are fp32, rounded once at the end.  A warp takes one token and a run of its heads, without a barrier in the CTA: it
 // works out the token's angles, in 64 bits (at position 10^6 an fp32 product is off by 0.03 rad), reduced to a fraction of a turn and
-// handed to sincospif, keeps cosines, sines and weights in registers as one factor an element, and goes through its heads with four rows
+// handed to sincospif in fp32 (off by 2^-26 of a turn, 1e-7 rad, at most: what fp32 sines are good for), keeps cosines, sines and weights in registers as one factor an element, and goes through its heads with four rows
 // per group of lanes on their way.
 // Measured: 8192 tokens of 32 + 8 heads of 128 in bf16, 30.7 us, 5.5 TB/s (with partners fetched by shuffles 36.2, with a branch for elements
-// that are not rotated 34.2); one token, and 224, 4.3 us (a launch).
+// that are not rotated 34.2); one token, and 224, 4.3 us (a launch).  The same bytes in the other forms: heads of 64 and 256 30.1 and 31.7,
+// pairs 30.0 to 31.9 (heads of 64, 128, 256), fp32 (4096 tokens) 29.8 to 31.2, in pairs 30.4 to 32.0.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -103,3 +103,56 @@ def test_layers_together_and_one_by_one(L, N):
         ref = O.quantise(x.double().cpu().numpy())
         ref[T - 3:] = 0
         assert np.array_equal(got.double().cpu().numpy(), ref)
+
+
+def test_plain_stream_order_gives_the_same_bits():
+    """A cycle of every call, with the library's overlap of kernels and without it, many times over: each call waits for what it reads."""
+    cx = ctx()
+    N, Ns = 12, 16
+    parent = np.array([W.tree_random(W.IntStream(W.stream_key(9, b)), N, 5) for b in range(B)], dtype=np.int32)
+    desc = cx.tree_desc(parent, slot=np.array([np.random.default_rng(b).permutation(Ns)[:N] for b in range(B)]), n_slots=Ns)
+    freq = (1e4 ** (-torch.arange(64, dtype=torch.float64) / 64)).float().cuda()
+    res = {}
+    try:
+        for on in (False, True):
+            cx.set_overlap(on)
+            rs = np.random.default_rng(8)
+            t = dict(table=filled(0, B + 1, 40), row_pages=filled(0, B + 1), refs=filled(0, 130), free_list=filled(0, 130), free_count=filled(0, 1),
+                     work=filled(0, binding.pages_work_ints(B + 1, 130)))
+            pool = torch.zeros(130, HKV, 2, P * 72, dtype=torch.uint8, device="cuda")
+            pt = binding.PageTable(page_size=P, pools=[pool], **t)
+            cx.pages_init(pt)
+            rows, ctx_len, ctx_next = i32([2, 0, 3]), i32([0, 0, 0]), i32([0, 0, 0])
+            qo, ko = (torch.empty(B, N, h, 128, dtype=torch.bfloat16, device="cuda") for h in (HQ, HKV))
+            out, work = torch.empty(B, N, HQ, 128, device="cuda"), torch.empty(cx.kv4_work_bytes(desc, HQ, HKV), dtype=torch.uint8, device="cuda")
+            st, acc, ln, node = filled(-1, B), filled(-1, B, 6), filled(0, B), i32(rs.integers(0, N, B))
+            state = torch.zeros(B + 1, 64, device="cuda")
+            state.copy_(torch.arange(B + 1, device="cuda")[:, None])
+            q, k, v = (bf16(rs.standard_normal((B, N, h, 128))) for h in (HQ, HKV, HKV))
+            layer = binding.Kv4Layer(Hq=HQ, Hkv=HKV, pages=pool, table=t["table"], page_size=P, refs=t["refs"], scale=128 ** -0.5, ctx_len=ctx_len, cache_row=rows,
+                                     q=qo, k_new=ko, v_new=v, out=out, status=st, work=work)
+            rope = binding.QkNormRope(q=q, k=k, q_out=qo, k_out=ko, inv_freq=freq, ctx_len=ctx_len)
+            blocks, packed, sums = binding.RowBlocks([state]), cx.pack_kv4([layer]), []
+            kb, vb = (torch.empty(B, HKV, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            for cycle in range(30):
+                cx.pages_reserve(pt, rows, ctx_len, add=Ns)
+                cx.qk_norm_rope(rope, desc)
+                cx.kv4_write_tree(desc, packed)
+                cx.kv4_attention(desc, packed)
+                cx.path_from_node(desc, node, 6, acc, ln)
+                cx.kv4_publish(desc, packed, acc, ln, ctx_next)
+                cx.pages_free(pt, rows, ctx_next)
+                cx.kv4_read(layer, rows, ctx_len, kb, vb)
+                cx.rows_copy(blocks, rows[:1], i32([1]))
+                if cycle % 5 == 4:
+                    cx.pages_compact(pt)
+                ctx_len.copy_(ctx_next)
+                sums.append((out.clone(), kb.clone(), vb.clone(), st.clone(), ctx_len.clone(), t["table"].clone(), state.clone()))
+            torch.cuda.synchronize()
+            res[on] = sums
+    finally:
+        cx.set_overlap(True)
+    assert all((s[3] == 0).all() for s in res[False]) and int(res[False][-1][4].sum()) > 30
+    for cycle, (a, b) in enumerate(zip(res[False], res[True])):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y), cycle
