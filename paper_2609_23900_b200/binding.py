@@ -239,6 +239,7 @@ def _listed(first: torch.Tensor, **tensors) -> int:
 
 
 _ANY = 1 << 62           # room of a tensor that is not given: the library says which ones a call needs
+_KV4_ROOM = ("ctx_len, cache_row or status", "q, out or lse", "k_new and v_new")       # a Kv4Layer's tensors by what a call counts in them
 
 
 def pages_work_ints(n_rows: int, n_pages: int) -> int:
@@ -410,42 +411,35 @@ class Context:
         """ctypes array of the layers' argument blocks (reusable across calls); keeps the layers, and knows how much their tensors hold."""
         arr = (_Kv4Args * len(layers))(*[l.args for l in layers])
         arr.layers = list(layers)
-        for name in ("sequences", "nodes", "new_tokens"):
-            setattr(arr, name, min((getattr(l, name) for l in layers), default=_ANY))
+        arr.room = tuple(min((l.room[i] for l in layers), default=_ANY) for i in range(len(_KV4_ROOM)))
         return arr
 
     @staticmethod
-    def _kv4(layers):
-        if not isinstance(layers, ctypes.Array):
-            return Context.pack_kv4(layers)
-        if not hasattr(layers, "layers"):
-            raise ValueError("an array of layers has to come from pack_kv4")
+    def _kv4(layers, sequences: int = 0, kind: int = 0, tokens: int = 0):
+        """Packed layers whose tensors hold a word for each of ``sequences`` and, of one kind of tensors, ``tokens`` tokens."""
+        room = getattr(layers, "room", None)
+        if room is None:
+            if isinstance(layers, ctypes.Array):
+                raise ValueError("an array of layers has to come from pack_kv4")
+            layers = Context.pack_kv4(layers)
+            room = layers.room
+        if sequences > room[0] or tokens > room[kind]:
+            i = 0 if sequences > room[0] else kind
+            raise ValueError(f"{_KV4_ROOM[i]} too small: room for {room[i]}, {sequences if i == 0 else tokens} needed")
         return layers
-
-    @staticmethod
-    def _kv4_on(desc: "TreeDesc", layers, nodes: Optional[str] = None):
-        """Packed layers whose tensors hold a word for each of desc's sequences and (``nodes``: which ones) a token for each of its nodes."""
-        arr = Context._kv4(layers)
-        if desc.B > arr.sequences:
-            raise ValueError("ctx_len, cache_row or status is too small for these trees")
-        if nodes is not None and desc.B * desc.N > getattr(arr, nodes):
-            raise ValueError(f"{'q, out or lse' if nodes == 'nodes' else 'k_new or v_new'} is too small for these trees")
-        return arr
 
     def kv4_work_bytes(self, desc: "TreeDesc", Hq: int, Hkv: int, n_splits: int = 0) -> int:
         """Bytes of workspace ``kv4_attention`` needs (Kv4Layer's ``work``)."""
         return int(_lib.lumo_kv4_work_bytes(self._h, desc._h, int(Hq), int(Hkv), int(n_splits)))
 
     def kv4_write_tree(self, desc: "TreeDesc", layers, stream=None):
-        arr = self._kv4_on(desc, layers, "new_tokens")
+        arr = self._kv4(layers, desc.B, 2, desc.nodes)
         self._check(_lib.lumo_kv4_write_tree(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_append(self, layers, tok_row: torch.Tensor, tok_pos: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None):
         """Entries of listed tokens (int32 rows and positions, [T]); ``status``, if given, gets a word per token."""
-        arr = self._kv4(layers)
         T = _listed(tok_row, tok_row=tok_row, tok_pos=tok_pos, status=status)
-        if T > arr.new_tokens:
-            raise ValueError(f"k_new and v_new hold {arr.new_tokens} tokens, {T} are listed")
+        arr = self._kv4(layers, 0, 2, T)
         self._check(_lib.lumo_kv4_append(self._h, arr, len(arr), T, _ptr(tok_row), _ptr(tok_pos), _ptr(status), _stream(stream)))
 
     def kv4_read(self, layer: "Kv4Layer", tok_row: torch.Tensor, tok_pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
@@ -459,16 +453,17 @@ class Context:
                                        _stream(stream)))
 
     def kv4_attention(self, desc: "TreeDesc", layers, stream=None):
-        arr = self._kv4_on(desc, layers, "nodes")
+        arr = self._kv4(layers, desc.B, 1, desc.nodes)
         self._check(_lib.lumo_kv4_attention(self._h, desc._h, arr, len(arr), _stream(stream)))
 
     def kv4_publish(self, desc: "TreeDesc", layers, accepted: torch.Tensor, length: torch.Tensor,
                     ctx_len_out: Optional[torch.Tensor] = None, stream=None):
-        arr = self._kv4_on(desc, layers)
-        if (accepted.dtype != torch.int32 or accepted.dim() != 2 or accepted.shape[0] < desc.B or length.dtype != torch.int32 or length.numel() < desc.B or
-                (ctx_len_out is not None and (ctx_len_out.dtype != torch.int32 or ctx_len_out.numel() < desc.B))):
+        arr = self._kv4(layers, desc.B)
+        shape, B = accepted.shape, desc.B
+        if (len(shape) != 2 or shape[0] < B or length.numel() < B or accepted.dtype != torch.int32 or length.dtype != torch.int32 or
+                ctx_len_out is not None and (ctx_len_out.numel() < B or ctx_len_out.dtype != torch.int32)):
             raise ValueError("accepted must be int32 [B, lmax], length and ctx_len_out int32 [B]")
-        self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), int(accepted.shape[1]),
+        self._check(_lib.lumo_kv4_publish(self._h, desc._h, arr, len(arr), _ptr(accepted), _ptr(length), shape[1],
                                           _ptr(ctx_len_out), _stream(stream)))
 
     # ---- pages ----
@@ -514,6 +509,7 @@ class TreeDesc:
         self.B, self.N = parent.shape
         slot_a = None if slot is None else np.ascontiguousarray(slot, dtype=np.int32)
         depth_a = None if depth is None else np.ascontiguousarray(depth, dtype=np.int32)
+        self.nodes = self.B * self.N
         self.Ns = int(n_slots) if n_slots is not None else self.N
         h = ctypes.c_void_p()
         rc = _lib.lumo_tree_desc_create(
@@ -702,11 +698,9 @@ class Kv4Layer:
             setattr(a, name, _ptr(self.tensors[name]))
         a.work_bytes = work.numel() * work.element_size() if work is not None else 0
         self.args = a
-        # what the tensors hold: words per sequence, tokens of the attention, tokens to write
+        # what the tensors hold, by _KV4_ROOM
         room = lambda per, *tensors: min((t.numel() // max(per, 1) for t in tensors if t is not None), default=_ANY)       # noqa: E731
-        self.sequences = room(1, ctx_len, cache_row, status)
-        self.nodes = min(room(int(Hq) * 128, q, out), room(int(Hq), lse))
-        self.new_tokens = room(int(Hkv) * 128, k_new, v_new)
+        self.room = (room(1, ctx_len, cache_row, status), min(room(int(Hq) * 128, q, out), room(int(Hq), lse)), room(int(Hkv) * 128, k_new, v_new))
 
 
 class PageTable:

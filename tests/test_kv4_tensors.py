@@ -99,7 +99,6 @@ def test_a_list_is_no_longer_than_the_keys(ctx):
     seven, five = B.Kv4Layer(**cache(), k_new=bf16(7, 2, 128), v_new=bf16(7, 2, 128)), B.Kv4Layer(**cache(), k_new=bf16(5, 2, 128), v_new=bf16(5, 2, 128))
     uneven = B.Kv4Layer(**cache(), k_new=bf16(9, 2, 128), v_new=bf16(6, 2, 128))
     tree = B.Kv4Layer(**cache(), k_new=bf16(2, 3, 2, 128), v_new=bf16(2, 3, 2, 128))
-    assert (seven.new_tokens, uneven.new_tokens, tree.new_tokens) == (7, 6, 6)
     for layer, n in ((seven, 7), (five, 5), (uneven, 6), (tree, 6)):
         for layers in ([layer], ctx.pack_kv4([layer])):
             reaches_launch(lambda: ctx.kv4_append(layers, i32(n), i32(n)))
