@@ -139,10 +139,10 @@ int lumo_ctx_set_scan_algo(lumo_ctx* ctx, int algo);
 
 /* Test aid for the failure path of the tensor-core scans and of the attention over the 4-bit cache.  They wait for their tensor-core work
  * (the streamed scan also for the state's copy, the attention for its tiles') on mbarriers with a bounded number of polls; when the
- * bound runs out they write LUMO_SEQ_TIMEOUT into the status words, free their tensor memory and return.  With the drill on, the solved scan (algorithm 3) and the
- * streamed scan (0 and 5, where they stream) and lumo_kv4_attention issue no asynchronous tensor-core work and no such copy (so nothing is in
- * flight) and poll only 1024 times: the waits run out by construction and the failure path executes, harmlessly.  The
- * other forms run as ever.  Outputs of such a call are undefined (a streamed commit_verify changes no state).  Default off. */
+ * bound runs out they write LUMO_SEQ_TIMEOUT into the status words, free their tensor memory and return.  With the drill on, the
+ * solved scan (algorithm 3), the streamed scan (0 and 5, where they stream) and lumo_kv4_attention issue no asynchronous tensor-core
+ * work and no such copy (so nothing is in flight) and poll only 1024 times: the waits run out by construction and the failure path
+ * executes, harmlessly.  The other forms run as ever.  Outputs of such a call are undefined (a streamed commit_verify changes no state).  Default off. */
 int lumo_ctx_set_timeout_drill(lumo_ctx* ctx, int on);
 
 /* Kernel overlap (default on): the kernels of every call are launched with programmatic dependent launch,

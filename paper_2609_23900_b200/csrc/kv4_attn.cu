@@ -38,7 +38,7 @@ namespace {
 //
 // Every warp has its own reference maximum per row and its own sums; they meet once per segment, through shared memory, in warp order.
 // A tile takes each scheduler 720 instructions (90 for 16 keys and scheduler; three quarters turn codes into f16), and the SM's share of the
-// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 56 to 59 us, 4.0 TB/s;
+// memory 800 cycles; four warps a scheduler issue in six cycles of ten, so a tile takes 1170.  Sixteen tokens at 16k: 57 to 58 us, 4.0 TB/s;
 // one token at 4k: 12.2 us, of which the attention kernel takes 8.2 (a chain of dependent loads, two tiles and the warps' meeting) and the
 // merge the rest.
 template <int NT> struct Small {

@@ -22,8 +22,8 @@
 // each scheduler issues 1390 instructions: no unit is full, but five warps a scheduler find something to issue in three cycles of four at
 // best.  The cache's bytes, 18 KB a tile, need 800 cycles of the SM's share of the memory.  Around the tiles a CTA spends 10 thousand cycles
 // until its first logits (lengths, page numbers, first copies and first instructions, one after another) and 4 to 6 thousand on the
-// read-out.  Measured, with the merge: 4 x 8 nodes at 8k 26.5 to 27.5 us, 8 x 28 at 16k 71 to 77 us (615 to 665 TFLOP/s, at the power limit's
-// edge; 66 in a short run), 64 nodes at 128k 162 us (845 TFLOP/s, at 1.64 GHz under the power limit).
+// read-out.  Measured, with the merge: 4 x 8 nodes at 8k 26.5 to 28 us, 8 x 28 at 16k 71 to 77 us (615 to 665 TFLOP/s, at the power limit's
+// edge; 66 in a short run), 64 nodes at 128k 161 to 164 us (840 to 855 TFLOP/s, at 1.64 GHz under the power limit).
 #include "f32x2.h"
 #include "kv4_attn.h"
 
